@@ -370,6 +370,107 @@ mgg_status_t mgg_layer_forward(const mgg_partition_t *p, const mgg_layer_desc_t 
                                mgg_dtype_t out_dtype, void *out, int64_t ld_out, void *stream);
 
 /* ---------------------------------------------------------------------------------------
+ * mgg_embed / mgg_embed_grad -- the lookup of single rows with ids that change from call to call (tokens, node
+ * numbers), scaled, and the gradient of the table.  Beside mgg_bag_sum, whose ids are laid out once on the host.
+ *
+ *     out[i] = scale * table[ids[i]]              an id outside [0, table_rows) (padding: -1) gives a row of zeros
+ *     grad_table[v] = scale * sum over i with ids[i] = v of grad_out[i]
+ *
+ * ids [n] DEVICE, id_type I32 or I64.  table [table_rows x dim], out [n x dim], grad_out [n x dim] and
+ * grad_table [table_rows x dim] DEVICE, F32 or BF16 each, leading dimensions >= dim; columns beyond dim are not
+ * touched.  Arithmetic is fp32, rounded once (nearest even) as a row is written.  No output may alias an input.
+ *
+ * mgg_embed_grad sorts the ids (stable), adds up the rows of an id in the order of their positions, in pieces whose size
+ * depends on n and dim alone, and uses no float atomics: the same call gives the same bits.  Ids outside the table
+ * carry no gradient.  accumulate 0: every row of grad_table is written, those that no id names with zeros; 1: the sums
+ * are added to what the rows hold, rows that no id names are not touched.  workspace is a DEVICE buffer of at
+ * least mgg_embed_grad_workspace_bytes() bytes, 256-byte aligned, that no other call uses at the same time.
+ * Both are asynchronous on `stream`, allocate nothing and can be captured into a graph.
+ * Errors: INVALID_ARG, UNSUPPORTED (more than 2^31 - 2 table rows; for the gradient also n beyond 2^30), HIP.
+ * ------------------------------------------------------------------------------------- */
+typedef enum { MGG_I32 = 0, MGG_I64 = 1 } mgg_index_t;
+
+mgg_status_t mgg_embed(int64_t n, mgg_index_t id_type, const void *ids, int64_t table_rows, mgg_dtype_t table_dtype,
+                       const void *table, int32_t dim, int64_t ld_table, float scale, mgg_dtype_t out_dtype, void *out,
+                       int64_t ld_out, void *stream);
+size_t       mgg_embed_grad_workspace_bytes(int64_t n, int64_t table_rows, int32_t dim);   /* 0 on bad arguments */
+mgg_status_t mgg_embed_grad(int64_t n, mgg_index_t id_type, const void *ids, int64_t table_rows, mgg_dtype_t grad_dtype,
+                            const void *grad_out, int32_t dim, int64_t ld_grad, float scale, int32_t accumulate,
+                            mgg_dtype_t out_dtype, void *grad_table, int64_t ld_table, void *workspace,
+                            size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------
+ * mgg_update_grouped / mgg_update_grouped_grad -- the Update with a weight matrix per group of rows (node types,
+ * experts), and its gradients.  Rows group_ptr[g] .. group_ptr[g + 1] - 1 belong to group g:
+ *
+ *     out[r] = act(a[r] . w[g] + bias[g])
+ *     dz = grad_out (act NONE), or grad_out where out > 0 and 0 elsewhere (act RELU)
+ *     grad_a[r] = dz[r] . w[g]^T,   grad_w[g] = sum over the group's rows of a[r]^T dz[r],   grad_bias[g] = sum of dz[r]
+ *
+ * group_ptr [n_groups + 1] is a DEVICE array (what a router counts there needs no copy to the host), ascending, within
+ * [0, n_rows]; offsets outside are taken as the nearest bound and a group whose end lies before its start as empty, so
+ * that no access leaves the buffers, but which rows of groups that overlap are written is then not defined.  Rows
+ * before the first group and behind the last are left as they were and are part of no sum; an empty group
+ * has a grad_w and grad_bias of zeros.  n_groups 1 with {0, n_rows} is the plain Update of mgg_update.
+ * a [n_rows x d_in], w [n_groups x d_in x d_out] contiguous, grad_out [n_rows x d_out]: DEVICE, one dtype for all, F32 or
+ * BF16.  bias, grad_bias [n_groups x d_out] DEVICE fp32 or NULL.  out, grad_a [n_rows x d_in], grad_w (like w): F32 or
+ * BF16 each.  Products are summed in fp32 (F32 operands on the fp32 matrix instruction) and rounded once as they
+ * are written.  Outputs must not alias inputs.  act is NONE or RELU.
+ *
+ * mgg_update_grouped_grad computes those of grad_a, grad_w and grad_bias that are not NULL; a is read for grad_w, w for
+ * grad_a and `out` (what the forward call wrote, of dtype out_dtype) for RELU only, and may be NULL otherwise.
+ * accumulate: MGG_ACC_W adds to what grad_w holds, MGG_ACC_BIAS to what grad_bias holds.  workspace: a DEVICE buffer of at
+ * least mgg_update_grouped_grad_workspace_bytes() bytes, 256-byte aligned, that no other call uses at the same time.
+ * Sums are made in an order that depends on the sizes and group_ptr alone: the same call gives the same bits.
+ * Both are asynchronous on `stream`, allocate nothing and can be captured into a graph (group_ptr may change between
+ * replays).  Errors: INVALID_ARG, UNSUPPORTED (softmax; a, w and grad_out of two dtypes; more than 2^31 - 1 rows,
+ * 2^16 - 1 groups or 2^22 columns or elements from row to row), HIP.
+ * ------------------------------------------------------------------------------------- */
+#define MGG_ACC_W 1
+#define MGG_ACC_BIAS 2
+
+mgg_status_t mgg_update_grouped(int64_t n_rows, int32_t n_groups, const int64_t *group_ptr, mgg_dtype_t a_dtype, const void *a,
+                                int64_t ld_a, int32_t d_in, mgg_dtype_t w_dtype, const void *w, const float *bias, int32_t d_out,
+                                mgg_act_t act, mgg_dtype_t out_dtype, void *out, int64_t ld_out, void *stream);
+/* 0 on bad arguments; good for every choice of outputs */
+size_t       mgg_update_grouped_grad_workspace_bytes(int64_t n_rows, int32_t n_groups, int32_t d_in, int32_t d_out, mgg_dtype_t dtype,
+                                                     mgg_act_t act);
+mgg_status_t mgg_update_grouped_grad(int64_t n_rows, int32_t n_groups, const int64_t *group_ptr, mgg_dtype_t dtype, const void *grad_out,
+                                     int64_t ld_grad, mgg_act_t act, mgg_dtype_t out_dtype, const void *out, int64_t ld_out,
+                                     const void *a, int64_t ld_a, int32_t d_in, const void *w, int32_t d_out,
+                                     mgg_dtype_t grad_a_dtype, void *grad_a, int64_t ld_grad_a, mgg_dtype_t grad_w_dtype, void *grad_w,
+                                     float *grad_bias, int32_t accumulate, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------
+ * mgg_distill_loss -- training against a teacher of which the top logits of each row are kept (a large network's
+ * answers for a small one's training): the divergence of the student's softmax from the teacher's at temperature T, and
+ * on request its gradient, from one reading of the logits.
+ *
+ *     p = softmax(top_logits[r] / T) over the row's present entries,   q = softmax(logits[r] / T) over all n_classes
+ *     loss[r] = row_weight[r] T^2 sum over the entries of p (log p - log q[their class])
+ *     grad_logits[r][c] = row_weight[r] T (q[c] - sum of p over the entries of class c)      (the gradient of sum_r loss[r])
+ *
+ * logits [n_rows x n_classes] F32 or BF16; top_ids [n_rows x k] I32 or I64 and top_logits [n_rows x k] F32 or BF16:
+ * DEVICE.  An entry whose id lies outside [0, n_classes) is not there (whatever its logit holds); one with a logit of
+ * -infinity has p = 0 and adds nothing.  Two entries of one class both count.  row_weight [n_rows] DEVICE fp32 or NULL (1).
+ * A row has loss 0 and a gradient of zeros where its weight is 0 (whatever its logits hold, NaN included), where no entry is
+ * left, and where all its logits are -infinity.  A class with logit -infinity has q = 0; the loss is infinite where the
+ * teacher gives it p > 0.  NaN or +infinity elsewhere give NaN in their row.
+ * loss [n_rows] DEVICE fp32.  grad_logits [n_rows x n_classes] F32 or BF16, or NULL: no gradient; it may be `logits`
+ * itself (same dtype and leading dimension) and must not overlap it otherwise.  Arithmetic is fp32, in a fixed order.
+ * workspace: a DEVICE buffer of at least mgg_distill_workspace_bytes() bytes, 256-byte aligned, that no other call uses
+ * at the same time.  Asynchronous on `stream`, allocates nothing, can be captured into a graph.
+ * Errors: INVALID_ARG (a temperature outside [1e-6, 1e6] among them), UNSUPPORTED (k above 1024, 2^31 - 1 classes
+ * or rows), HIP.
+ * ------------------------------------------------------------------------------------- */
+size_t       mgg_distill_workspace_bytes(int64_t n_rows, int32_t n_classes);   /* 0 on bad arguments */
+mgg_status_t mgg_distill_loss(int64_t n_rows, int32_t n_classes, mgg_dtype_t logits_dtype, const void *logits, int64_t ld_logits,
+                              int32_t k, mgg_index_t id_type, const void *top_ids, int64_t ld_ids, mgg_dtype_t top_dtype,
+                              const void *top_logits, int64_t ld_top, float temperature, const float *row_weight, float *loss,
+                              mgg_dtype_t grad_dtype, void *grad_logits, int64_t ld_grad, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------
  * mgg_split_edge_balanced -- section 4.1 Step-1 / Algorithm 1: contiguous node ranges with
  * about ceil(E / num_parts) edges each.  Host only.  bounds_out has num_parts+1 entries,
  * bounds_out[0] = 0, bounds_out[num_parts] = num_nodes; interior point s is the first node

@@ -17,6 +17,8 @@ LIB_PATH = os.path.join(_HERE, "libmgg.so")
 
 OK, ERR_INVALID_ARG, ERR_BAD_GRAPH, ERR_UNSUPPORTED, ERR_ALLOC, ERR_HIP = range(6)
 F32, BF16 = 0, 1
+I32, I64 = 0, 1
+ACC_W, ACC_BIAS = 1, 2
 AGG_GCN_SYM, AGG_GIN_SUM = 0, 1
 ACT_NONE, ACT_RELU, ACT_SOFTMAX = 0, 1, 2
 _MODE = {"gcn": AGG_GCN_SYM, "gin": AGG_GIN_SUM}
@@ -32,6 +34,8 @@ EXPORTED_SYMBOLS = [
     "mgg_split_edge_balanced", "mgg_set_option", "mgg_get_option", "mgg_partition_set_option", "mgg_partition_get_option", "mgg_time_aggregate", "mgg_probe_gather",
     "mgg_model_evaluate", "mgg_tuner_create", "mgg_tuner_set_constraint", "mgg_tuner_next", "mgg_tuner_report", "mgg_tuner_result",
     "mgg_tuner_table", "mgg_tuner_destroy", "mgg_tune_aggregate",
+    "mgg_embed", "mgg_embed_grad", "mgg_embed_grad_workspace_bytes", "mgg_update_grouped", "mgg_update_grouped_grad",
+    "mgg_update_grouped_grad_workspace_bytes", "mgg_distill_loss", "mgg_distill_workspace_bytes",
     "mgg_last_error", "mgg_version",
 ]
 
@@ -111,6 +115,7 @@ def lib():
         # handles and device pointers handed to the library must belong to that runtime
         import torch
         _DTYPE_CODE.update({torch.float32: F32, torch.bfloat16: BF16})
+        _INDEX_CODE.update({torch.int32: I32, torch.int64: I64})
         L = C.CDLL(LIB_PATH)
         L.mgg_last_error.restype = C.c_char_p
         L.mgg_version.restype = C.c_char_p
@@ -169,6 +174,24 @@ def lib():
                                          C.c_void_p, C.c_int, C.c_float, C.c_int, C.c_void_p, C.c_void_p, C.c_int32,
                                          C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p,
                                          C.POINTER(Knobs), C.POINTER(C.c_double)]
+        L.mgg_embed.argtypes = [C.c_int64, C.c_int, C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_int,
+                                C.c_void_p, C.c_int64, C.c_void_p]
+        L.mgg_embed_grad_workspace_bytes.restype = C.c_size_t
+        L.mgg_embed_grad_workspace_bytes.argtypes = [C.c_int64, C.c_int64, C.c_int32]
+        L.mgg_embed_grad.argtypes = [C.c_int64, C.c_int, C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_int32,
+                                     C.c_int, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.mgg_update_grouped.argtypes = [C.c_int64, C.c_int32, C.c_void_p, C.c_int, C.c_void_p, C.c_int64, C.c_int32, C.c_int, C.c_void_p,
+                                         C.c_void_p, C.c_int32, C.c_int, C.c_int, C.c_void_p, C.c_int64, C.c_void_p]
+        L.mgg_update_grouped_grad_workspace_bytes.restype = C.c_size_t
+        L.mgg_update_grouped_grad_workspace_bytes.argtypes = [C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int, C.c_int]
+        L.mgg_update_grouped_grad.argtypes = [C.c_int64, C.c_int32, C.c_void_p, C.c_int, C.c_void_p, C.c_int64, C.c_int, C.c_int, C.c_void_p,
+                                              C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int32, C.c_int, C.c_void_p, C.c_int64,
+                                              C.c_int, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.mgg_distill_workspace_bytes.restype = C.c_size_t
+        L.mgg_distill_workspace_bytes.argtypes = [C.c_int64, C.c_int32]
+        L.mgg_distill_loss.argtypes = [C.c_int64, C.c_int32, C.c_int, C.c_void_p, C.c_int64, C.c_int32, C.c_int, C.c_void_p, C.c_int64, C.c_int,
+                                       C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int64, C.c_void_p,
+                                       C.c_size_t, C.c_void_p]
         _lib = L
     return _lib
 
@@ -190,6 +213,9 @@ def _np_ptr(a: Optional[np.ndarray]):
 # Marshalling is what the smallest calls spend their time on (a layer of a 4 k-node graph: two launches of a few
 # microseconds each), so these avoid ctypes objects and torch's stream wrapper where a plain int does.
 _DTYPE_CODE = {}                # torch dtype -> mgg_dtype_t, filled when the library is loaded
+
+
+_INDEX_CODE = {}                # the same for mgg_index_t
 
 
 def _torch_dtype_code(t) -> int:
@@ -557,6 +583,217 @@ def mgg_layer_forward(part: Partition, mode: str, x_local, x_halo, weights, acts
                                    _dev_ptr(x_halo), _ld(x_local), _dev_ptr(workspace), workspace.numel(),
                                    _torch_dtype_code(out), _dev_ptr(out), _ld(out), _stream(stream)))
     return out
+
+
+# ------------------------------------------------------------------------------- training
+# Lookup, grouped Update and distillation loss.  What the C ABI cannot see is checked here: shapes, dtypes, and that every
+# tensor lives on the current device (whose stream the call goes to).
+def _same_device(*tensors):
+    import torch
+    device = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise TypeError("device tensor expected")
+        if device is None:
+            device = t.device
+            if device.index != torch.cuda.current_device():
+                raise ValueError(f"tensors live on {device}, the current device is cuda:{torch.cuda.current_device()}")
+        elif t.device != device:
+            raise ValueError(f"tensors live on {device} and on {t.device}")
+    return device
+
+
+def _code(dtype) -> int:
+    lib()
+    code = _DTYPE_CODE.get(dtype)
+    if code is None:
+        raise TypeError(f"unsupported tensor dtype {dtype}")
+    return code
+
+
+def _index_code(t) -> int:
+    lib()
+    code = _INDEX_CODE.get(t.dtype)
+    if code is None:
+        raise TypeError(f"int32 or int64 ids expected, got {t.dtype}")
+    return code
+
+
+def _new(shape, dtype, device, stream):
+    """A tensor that belongs to the stream the call goes to: memory freed there is not given to work on another one."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _workspace(workspace, need: int, device, stream):
+    import torch
+    if workspace is None:
+        return _new((max(need, 1),), torch.uint8, device, stream)
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return workspace
+
+
+def _shape(name: str, t, rows: int, cols: int):
+    if t is not None and (t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols):
+        raise ValueError(f"{name} must be {rows} x {cols}, got {tuple(t.shape)}")
+
+
+def _ids_1d(ids):
+    if ids.dim() != 1 or (ids.shape[0] > 1 and ids.stride(0) != 1):
+        raise ValueError("ids must be a contiguous 1-D tensor")
+    return _index_code(ids)
+
+
+def mgg_embed(ids, table, *, scale: float = 1.0, out=None, out_dtype=None, stream=None):
+    """out[i] = scale * table[ids[i]]; an id outside the table (padding) gives a row of zeros.  The output has the table's
+    dtype unless `out` or `out_dtype` says otherwise."""
+    id_type = _ids_1d(ids)
+    n, rows, dim = int(ids.shape[0]), int(table.shape[0]), int(table.shape[1])
+    device = _same_device(ids, table, out)
+    if out is None:
+        out = _new((n, dim), out_dtype or table.dtype, device, stream)
+    _shape("out", out, n, dim)
+    _check(lib().mgg_embed(n, id_type, ids.data_ptr(), rows, _code(table.dtype), table.data_ptr(), dim, _ld(table), scale, _code(out.dtype),
+                           out.data_ptr(), _ld(out), _stream(stream)))
+    return out
+
+
+def mgg_embed_grad_workspace_bytes(n: int, table_rows: int, dim: int) -> int:
+    return int(lib().mgg_embed_grad_workspace_bytes(int(n), int(table_rows), int(dim)))
+
+
+def mgg_embed_grad(ids, grad_out, table_rows: int, *, scale: float = 1.0, out=None, out_dtype=None, accumulate: bool = False, workspace=None,
+                   stream=None):
+    """The gradient [table_rows x dim] of mgg_embed's table, fp32 unless `out` or `out_dtype` says otherwise; accumulate adds to
+    `out` and leaves rows that no id names alone."""
+    import torch
+    id_type = _ids_1d(ids)
+    n, dim = int(ids.shape[0]), int(grad_out.shape[1])
+    _shape("grad_out", grad_out, n, dim)
+    device = _same_device(ids, grad_out, out, workspace)
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs `out`")
+        out = _new((table_rows, dim), out_dtype or torch.float32, device, stream)
+    _shape("out", out, table_rows, dim)
+    workspace = _workspace(workspace, mgg_embed_grad_workspace_bytes(n, table_rows, dim), device, stream)
+    _check(lib().mgg_embed_grad(n, id_type, ids.data_ptr(), table_rows, _code(grad_out.dtype), grad_out.data_ptr(), dim, _ld(grad_out), scale,
+                                int(accumulate), _code(out.dtype), out.data_ptr(), _ld(out), workspace.data_ptr(),
+                                workspace.numel() * workspace.element_size(), _stream(stream)))
+    return out
+
+
+def _check_groups(group_ptr, w, n_groups: int):
+    import torch
+    if group_ptr.dtype != torch.int64 or group_ptr.dim() != 1 or group_ptr.shape[0] < 1 or not group_ptr.is_contiguous():
+        raise ValueError("group_ptr must be a contiguous int64 tensor of n_groups + 1 offsets")
+    if w.dim() != 3 or w.shape[0] != n_groups or not w.is_contiguous():
+        raise ValueError(f"w must be a contiguous [{n_groups} x d_in x d_out] tensor, got {tuple(w.shape)}")
+
+
+def _check_bias(name: str, bias, n_groups: int, d_out: int):
+    import torch
+    if bias is not None and (bias.dtype != torch.float32 or tuple(bias.shape) != (n_groups, d_out) or not bias.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous fp32 [{n_groups} x {d_out}] tensor")
+
+
+def mgg_update_grouped(group_ptr, a, w, bias=None, act: str = "none", *, out=None, out_dtype=None, stream=None):
+    """out[r] = act(a[r] @ w[g] + bias[g]) for the rows group_ptr[g] <= r < group_ptr[g + 1] of every group g; other rows of
+    `out` are left as they are.  The output has a's dtype unless `out` or `out_dtype` says otherwise."""
+    n_groups = int(group_ptr.shape[0]) - 1
+    _check_groups(group_ptr, w, n_groups)
+    n, d_in, d_out = int(a.shape[0]), int(w.shape[1]), int(w.shape[2])
+    _shape("a", a, n, d_in)
+    _check_bias("bias", bias, n_groups, d_out)
+    device = _same_device(group_ptr, a, w, bias, out)
+    if out is None:
+        out = _new((n, d_out), out_dtype or a.dtype, device, stream)
+    _shape("out", out, n, d_out)
+    _check(lib().mgg_update_grouped(n, n_groups, group_ptr.data_ptr(), _code(a.dtype), a.data_ptr(), _ld(a), d_in, _code(w.dtype), w.data_ptr(),
+                                    _dev_ptr(bias), d_out, _ACT[act], _code(out.dtype), out.data_ptr(), _ld(out), _stream(stream)))
+    return out
+
+
+def mgg_update_grouped_grad_workspace_bytes(n_rows: int, n_groups: int, d_in: int, d_out: int, dtype, *, act: str = "none") -> int:
+    return int(lib().mgg_update_grouped_grad_workspace_bytes(int(n_rows), int(n_groups), int(d_in), int(d_out), _code(dtype), _ACT[act]))
+
+
+def mgg_update_grouped_grad(group_ptr, grad_out, a, w, act: str = "none", *, out=None, need_a: bool = True, need_w: bool = True, need_bias: bool = False,
+                            grad_a=None, grad_w=None, grad_bias=None, w_grad_dtype=None, accumulate: bool = False, workspace=None, stream=None):
+    """Gradients of mgg_update_grouped: (grad_a, grad_w), and grad_bias behind them with need_bias; None in the place of one that
+    is not needed.  `out` is what the forward call wrote (act "relu" only).  grad_a has a's dtype, grad_w fp32 unless
+    `w_grad_dtype` says otherwise; accumulate adds to the grad_w and grad_bias that are given."""
+    import torch
+    n_groups = int(group_ptr.shape[0]) - 1
+    _check_groups(group_ptr, w, n_groups)
+    n, d_in, d_out = int(a.shape[0]), int(w.shape[1]), int(w.shape[2])
+    _shape("a", a, n, d_in)
+    _shape("grad_out", grad_out, n, d_out)
+    if a.dtype != w.dtype or grad_out.dtype != w.dtype:
+        raise MggError(ERR_UNSUPPORTED, f"a, w and grad_out must have one dtype, got {a.dtype}, {w.dtype} and {grad_out.dtype}")
+    if act == "relu" and out is None:
+        raise ValueError("the gradient of a ReLU needs the forward call's `out`")
+    if act == "relu":
+        _shape("out", out, n, d_out)
+    device = _same_device(group_ptr, grad_out, a, w, out if act == "relu" else None, grad_a, grad_w, grad_bias, workspace)
+    add = (ACC_W if accumulate and grad_w is not None else 0) | (ACC_BIAS if accumulate and grad_bias is not None else 0)
+    if need_a and grad_a is None:
+        grad_a = _new((n, d_in), a.dtype, device, stream)
+    if need_w and grad_w is None:
+        grad_w = _new((n_groups, d_in, d_out), w_grad_dtype or torch.float32, device, stream)
+    if need_bias and grad_bias is None:
+        grad_bias = _new((n_groups, d_out), torch.float32, device, stream)
+    _shape("grad_a", grad_a, n, d_in)
+    if grad_w is not None and (tuple(grad_w.shape) != tuple(w.shape) or not grad_w.is_contiguous()):
+        raise ValueError(f"grad_w must be contiguous and {tuple(w.shape)}, got {tuple(grad_w.shape)}")
+    _check_bias("grad_bias", grad_bias, n_groups, d_out)
+    relu_out = out if act == "relu" else None
+    workspace = _workspace(workspace, mgg_update_grouped_grad_workspace_bytes(n, n_groups, d_in, d_out, w.dtype, act=act), device, stream)
+    _check(lib().mgg_update_grouped_grad(
+        n, n_groups, group_ptr.data_ptr(), _code(w.dtype), grad_out.data_ptr(), _ld(grad_out), _ACT[act],
+        F32 if relu_out is None else _code(relu_out.dtype), _dev_ptr(relu_out), 0 if relu_out is None else _ld(relu_out), a.data_ptr(), _ld(a), d_in,
+        w.data_ptr(), d_out, F32 if grad_a is None else _code(grad_a.dtype), _dev_ptr(grad_a), 0 if grad_a is None else _ld(grad_a),
+        F32 if grad_w is None else _code(grad_w.dtype), _dev_ptr(grad_w), _dev_ptr(grad_bias), add, workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream(stream)))
+    return (grad_a, grad_w, grad_bias) if need_bias or grad_bias is not None else (grad_a, grad_w)
+
+
+def mgg_distill_workspace_bytes(n_rows: int, n_classes: int) -> int:
+    return int(lib().mgg_distill_workspace_bytes(int(n_rows), int(n_classes)))
+
+
+def mgg_distill_loss(logits, top_ids, top_logits, *, temperature: float = 1.0, row_weight=None, need_grad: bool = False, grad=None, grad_dtype=None,
+                     loss=None, workspace=None, stream=None):
+    """Per-row divergence of the student's softmax(logits / T) from the softmax of the teacher's top logits, times T^2 and the row's
+    weight; with need_grad (or `grad`) also the gradient of the losses' sum, in the logits' dtype unless `grad` or `grad_dtype`
+    says otherwise.  `grad` may be `logits` itself.  Returns loss, or (loss, grad)."""
+    import torch
+    n, classes, k = int(logits.shape[0]), int(logits.shape[1]), int(top_ids.shape[1])
+    _shape("top_ids", top_ids, n, k)
+    _shape("top_logits", top_logits, n, k)
+    id_type = _index_code(top_ids)
+    if row_weight is not None and (row_weight.dtype != torch.float32 or tuple(row_weight.shape) != (n,) or not row_weight.is_contiguous()):
+        raise ValueError(f"row_weight must be a contiguous fp32 tensor of {n} values")
+    if loss is not None and (loss.dtype != torch.float32 or tuple(loss.shape) != (n,) or not loss.is_contiguous()):
+        raise ValueError(f"loss must be a contiguous fp32 tensor of {n} values")
+    device = _same_device(logits, top_ids, top_logits, row_weight, grad, loss, workspace)
+    if loss is None:
+        loss = _new((n,), torch.float32, device, stream)
+    if grad is None and need_grad:
+        grad = _new((n, classes), grad_dtype or logits.dtype, device, stream)
+    _shape("grad", grad, n, classes)
+    workspace = _workspace(workspace, mgg_distill_workspace_bytes(n, classes), device, stream)
+    _check(lib().mgg_distill_loss(n, classes, _code(logits.dtype), logits.data_ptr(), _ld(logits), k, id_type, top_ids.data_ptr(), _ld(top_ids),
+                                  _code(top_logits.dtype), top_logits.data_ptr(), _ld(top_logits), temperature, _dev_ptr(row_weight), loss.data_ptr(),
+                                  F32 if grad is None else _code(grad.dtype), _dev_ptr(grad), 0 if grad is None else _ld(grad), workspace.data_ptr(),
+                                  workspace.numel() * workspace.element_size(), _stream(stream)))
+    return loss if grad is None else (loss, grad)
 
 
 # ------------------------------------------------------------------------------- model and tuner

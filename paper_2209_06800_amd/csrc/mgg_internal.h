@@ -176,4 +176,46 @@ mgg_status_t probe_gather(int64_t table_bytes, int32_t row_bytes, int64_t n_gath
 // in place: x[i][:] = softmax(x[i][:]) for every row (update.hip)
 mgg_status_t launch_row_softmax(int64_t n_rows, int32_t d, mgg_dtype_t dtype, void *x, int64_t ld, hipStream_t stream);
 
+
+// lookup and its gradient (lookup.hip)
+mgg_status_t launch_embed(int64_t n, mgg_index_t id_type, const void *ids, int64_t table_rows, mgg_dtype_t table_dtype, const void *table, int32_t dim,
+                          int64_t ld_table, float scale, mgg_dtype_t out_dtype, void *out, int64_t ld_out, hipStream_t stream);
+size_t embed_grad_workspace(int64_t n, int64_t table_rows, int32_t dim);
+mgg_status_t launch_embed_grad(int64_t n, mgg_index_t id_type, const void *ids, int64_t table_rows, mgg_dtype_t grad_dtype, const void *grad, int32_t dim,
+                               int64_t ld_grad, float scale, bool accumulate, mgg_dtype_t out_dtype, void *out, int64_t ld_out, void *workspace,
+                               hipStream_t stream);
+
+// the Update by groups of rows (grouped.hip)
+struct GroupedGrad {
+    int64_t n_rows;
+    int32_t n_groups, d_in, d_out;
+    const int64_t *group_ptr;
+    mgg_dtype_t dtype, out_dtype, grad_a_dtype, grad_w_dtype;
+    const void *grad_out, *out, *a, *w;
+    int64_t ld_grad, ld_out, ld_a, ld_grad_a;
+    bool relu, add_w, add_bias;
+    void *grad_a, *grad_w;
+    float *grad_bias;
+};
+mgg_status_t launch_update_grouped(int64_t n_rows, int32_t n_groups, const int64_t *group_ptr, mgg_dtype_t dtype, const void *a, int64_t ld_a, int32_t d_in,
+                                   const void *w, const float *bias, int32_t d_out, bool relu, mgg_dtype_t out_dtype, void *out, int64_t ld_out,
+                                   hipStream_t stream);
+size_t grouped_grad_workspace(int64_t n_rows, int32_t n_groups, int32_t d_in, int32_t d_out, mgg_dtype_t dtype, bool relu);
+mgg_status_t launch_update_grouped_grad(const GroupedGrad &q, void *workspace, hipStream_t stream);
+
+// the loss against a teacher's top logits (distill.hip)
+struct Distill {
+    int64_t n_rows, ld_logits, ld_ids, ld_top, ld_grad;
+    int32_t n_classes, k;
+    mgg_dtype_t logits_dtype, top_dtype, grad_dtype;
+    mgg_index_t id_type;
+    const void *logits, *top_ids, *top_logits;
+    const float *row_weight;
+    float temperature;
+    float *loss;
+    void *grad;
+};
+size_t distill_workspace(int64_t n_rows, int32_t n_classes);
+mgg_status_t launch_distill(const Distill &q, void *workspace, hipStream_t stream);
+
 }  // namespace mgg
