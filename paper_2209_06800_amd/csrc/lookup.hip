@@ -87,28 +87,137 @@ hipError_t embed_typed(int64_t n, const void *ids, int64_t table_rows, const voi
 
 // ---- the ids in order ----------------------------------------------------------------------------------------
 // A stable radix sort of (id, position), least significant digit first; an id outside the table has the key table_rows,
-// behind all others.  Per digit: counts per block, their prefix sums over the blocks, and the scatter.
-constexpr int kDigitBits = 8, kBins = 1 << kDigitBits;
-constexpr int kPerThread = 16, kTile = kThreads * kPerThread;
+// behind all others.  The work is small beside the sums (8 bytes an id), so what counts is the number of launches: up to
+// kSmall ids one block sorts them in LDS; beyond, a digit takes two launches (counts per block; the scatter, whose blocks add up
+// the counts of the blocks before them), three where there are more blocks than that pays for.
+constexpr int kDigitBits = 9, kBins = 1 << kDigitBits;
+constexpr int kPerThread = 8, kTile = kThreads * kPerThread;
+constexpr int kScanTiles = 256;                     // up to so many blocks the scatter adds up their counts itself
+constexpr int kSmallThreads = 1024, kSmallBits = 8, kSmall = kSmallThreads * 8;
 
 struct SortArgs {
     const void *ids;                    // of the first pass
     const uint32_t *key_in, *pos_in;    // of the others
     uint32_t *key_out, *pos_out;
-    uint32_t *count;                    // [kBins x tiles]: per digit and block, then its exclusive prefix over the blocks
-    uint32_t *total;                    // [kBins]
+    uint32_t *count;                    // [tiles x kBins]: per block and digit, then, after the scan, those of the blocks before
+    uint32_t *total;                    // [kBins], written by the scan
     int64_t n, table_rows;
-    int32_t tiles, shift, bits;
+    int32_t tiles, shift, bits, passes;
 };
 
+template <typename Id>
+__device__ __forceinline__ uint32_t id_key(const SortArgs &p, int64_t i)
+{
+    const int64_t id = static_cast<const Id *>(p.ids)[i];
+    return id >= 0 && id < p.table_rows ? static_cast<uint32_t>(id) : static_cast<uint32_t>(p.table_rows);
+}
 template <typename Id, bool FIRST>
 __device__ __forceinline__ uint32_t sort_key(const SortArgs &p, int64_t i)
 {
-    if constexpr (FIRST) {
-        const int64_t id = static_cast<const Id *>(p.ids)[i];
-        return id >= 0 && id < p.table_rows ? static_cast<uint32_t>(id) : static_cast<uint32_t>(p.table_rows);
-    } else {
-        return p.key_in[i];
+    if constexpr (FIRST) return id_key<Id>(p, i);
+    else return p.key_in[i];
+}
+
+// The rank of this lane's key among those of its wavefront with the same digit: those of earlier steps, counted in
+// `seen`, and of earlier lanes.
+__device__ __forceinline__ uint32_t wave_rank(uint32_t *seen, uint32_t digit, int bits, bool there, int lane)
+{
+    uint64_t peers = __ballot(there);
+    for (int b = 0; b < bits; ++b) {
+        const bool set = (digit >> b) & 1u;
+        const uint64_t with = __ballot(set);
+        peers &= set ? with : ~with;
+    }
+    const int leader = there ? __ffsll(static_cast<unsigned long long>(peers)) - 1 : lane;
+    uint32_t old = 0;
+    if (there && lane == leader) old = atomicAdd(&seen[digit], static_cast<uint32_t>(__popcll(peers)));
+    old = __shfl(old, leader);
+    return old + static_cast<uint32_t>(__popcll(peers & ((1ull << lane) - 1)));
+}
+
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v, int lane)
+{
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) {
+        const uint32_t o = __shfl_up(v, off);
+        if (lane >= off) v += o;
+    }
+    return v;
+}
+
+// exclusive prefix sums of one value per thread; part: a word per wavefront
+template <int THREADS>
+__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t *part)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t incl = wave_scan(v, lane);
+    if (lane == 63) part[wave] = incl;
+    __syncthreads();
+    uint32_t before = incl - v;
+#pragma unroll
+    for (int w = 0; w < THREADS / kWave; ++w)
+        if (w < wave) before += part[w];
+    return before;
+}
+
+template <typename Id>
+__global__ __launch_bounds__(kSmallThreads) void sort_small_kernel(const SortArgs p)
+{
+    constexpr int kWaves = kSmallThreads / kWave, kB = 1 << kSmallBits;
+    __shared__ uint32_t key_at[kSmall], pos_at[kSmall];
+    __shared__ uint32_t seen[kWaves][kB];
+    __shared__ uint32_t part[kWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = static_cast<int>(p.n);
+    const int steps = (n + kSmallThreads - 1) / kSmallThreads;          // of a wavefront: it takes steps * 64 keys in a row
+    const int first = wave * steps * kWave + lane;
+    uint32_t key[8], pos[8], rank[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+        const int i = first + r * kWave;
+        if (r < steps && i < n) { key[r] = id_key<Id>(p, i); pos[r] = static_cast<uint32_t>(i); }
+    }
+    for (int pass = 0; pass < p.passes; ++pass) {
+        const int shift = pass * p.bits;
+        const uint32_t mask = (1u << p.bits) - 1;
+        for (int b = threadIdx.x; b < kWaves * kB; b += kSmallThreads) seen[b / kB][b % kB] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+            if (r < steps) rank[r] = wave_rank(seen[wave], (key[r] >> shift) & mask, p.bits, first + r * kWave < n, lane);
+        __syncthreads();
+        uint32_t sum = 0;
+        if (threadIdx.x < kB) {
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) sum += seen[w][threadIdx.x];
+        }
+        uint32_t start = block_scan<kSmallThreads>(sum, part);
+        if (threadIdx.x < kB) {
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const uint32_t c = seen[w][threadIdx.x];
+                seen[w][threadIdx.x] = start;
+                start += c;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+            if (r < steps && first + r * kWave < n) {
+                const uint32_t to = seen[wave][(key[r] >> shift) & mask] + rank[r];
+                key_at[to] = key[r];
+                pos_at[to] = pos[r];
+            }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            const int i = first + r * kWave;
+            if (r < steps && i < n) { key[r] = key_at[i]; pos[r] = pos_at[i]; }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+        const int i = first + r * kWave;
+        if (r < steps && i < n) { p.key_out[i] = key[r]; p.pos_out[i] = pos[r]; }
     }
 }
 
@@ -116,61 +225,54 @@ template <typename Id, bool FIRST>
 __global__ __launch_bounds__(kThreads) void sort_count_kernel(const SortArgs p)
 {
     __shared__ uint32_t bins[kBins];
-    bins[threadIdx.x] = 0;
+    for (int b = threadIdx.x; b < kBins; b += kThreads) bins[b] = 0;
     __syncthreads();
     const int64_t first = static_cast<int64_t>(blockIdx.x) * kTile;
-#pragma unroll 4
+#pragma unroll
     for (int r = 0; r < kPerThread; ++r) {
         const int64_t i = first + r * kThreads + threadIdx.x;
         if (i < p.n) atomicAdd(&bins[(sort_key<Id, FIRST>(p, i) >> p.shift) & ((1u << p.bits) - 1)], 1u);
     }
     __syncthreads();
-    p.count[static_cast<int64_t>(threadIdx.x) * p.tiles + blockIdx.x] = bins[threadIdx.x];
+    for (int b = threadIdx.x; b < kBins; b += kThreads) p.count[static_cast<int64_t>(blockIdx.x) * kBins + b] = bins[b];
 }
 
-// a block per digit: counts of the blocks -> exclusive prefix sums
+// counts of the blocks -> those of the blocks before: a thread per digit, wavefront w taking a quarter of the blocks
 __global__ __launch_bounds__(kThreads) void sort_scan_kernel(const SortArgs p)
 {
-    __shared__ uint32_t part[kThreads / kWave];
-    uint32_t *row = p.count + static_cast<int64_t>(blockIdx.x) * p.tiles;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int kWaves = kThreads / kWave;
+    __shared__ uint32_t part[kWaves][kWave];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = blockIdx.x * kWave + lane;
+    const int share = (p.tiles + kWaves - 1) / kWaves, from = wave * share, to = from + share < p.tiles ? from + share : p.tiles;
+    uint32_t sum = 0;
+#pragma unroll 8
+    for (int t = from; t < to; ++t) sum += p.count[static_cast<int64_t>(t) * kBins + b];
+    part[wave][lane] = sum;
+    __syncthreads();
     uint32_t before = 0;
-    for (int base = 0; base < p.tiles; base += kThreads) {
-        const int t = base + threadIdx.x;
-        const uint32_t c = t < p.tiles ? row[t] : 0u;
-        uint32_t incl = c;
 #pragma unroll
-        for (int off = 1; off < kWave; off <<= 1) {
-            const uint32_t o = __shfl_up(incl, off);
-            if (lane >= off) incl += o;
-        }
-        if (lane == 63) part[wave] = incl;
-        __syncthreads();
-        uint32_t prev = before, all = 0;
-#pragma unroll
-        for (int w = 0; w < kThreads / kWave; ++w) {
-            if (w < wave) prev += part[w];
-            all += part[w];
-        }
-        if (t < p.tiles) row[t] = prev + incl - c;
-        before += all;
-        __syncthreads();
+    for (int w = 0; w < kWaves; ++w)
+        if (w < wave) before += part[w][lane];
+    for (int t = from; t < to; ++t) {
+        uint32_t *c = p.count + static_cast<int64_t>(t) * kBins + b;
+        const uint32_t mine = *c;
+        *c = before;
+        before += mine;
     }
-    if (threadIdx.x == 0) p.total[blockIdx.x] = before;
+    if (wave == kWaves - 1) p.total[b] = before;
 }
 
 // Wave w of a block takes a quarter of its keys in order, 64 at a time; the place of a key is the digit's start + the keys of
 // the digit in earlier blocks + in earlier waves + in earlier steps of the wave + in earlier lanes of the step.
-template <typename Id, bool FIRST>
+template <typename Id, bool FIRST, bool SCANNED>
 __global__ __launch_bounds__(kThreads) void sort_scatter_kernel(const SortArgs p)
 {
-    constexpr int kWaves = kThreads / kWave;
+    constexpr int kWaves = kThreads / kWave, kPer = kBins / kThreads;
     __shared__ uint32_t seen[kWaves][kBins];
     __shared__ uint32_t part[kWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) seen[w][threadIdx.x] = 0;
-    __syncthreads();
+    const uint32_t mask = (1u << p.bits) - 1;
+    for (int b = threadIdx.x; b < kWaves * kBins; b += kThreads) seen[b / kBins][b % kBins] = 0;
     const int64_t first = static_cast<int64_t>(blockIdx.x) * kTile + wave * (kTile / kWaves) + lane;
     uint32_t key[kPerThread], rank[kPerThread];
 #pragma unroll
@@ -178,42 +280,45 @@ __global__ __launch_bounds__(kThreads) void sort_scatter_kernel(const SortArgs p
         const int64_t i = first + r * kWave;
         key[r] = i < p.n ? sort_key<Id, FIRST>(p, i) : 0u;
     }
+    // thread t holds digits kPer t .. kPer t + kPer - 1: all their keys, and those of the blocks before
+    uint32_t before[kPer], total[kPer];
 #pragma unroll
-    for (int r = 0; r < kPerThread; ++r) {
-        const bool there = first + r * kWave < p.n;
-        const uint32_t digit = (key[r] >> p.shift) & ((1u << p.bits) - 1);
-        uint64_t peers = __ballot(there);
-        for (int b = 0; b < p.bits; ++b) {
-            const bool set = (digit >> b) & 1u;
-            const uint64_t with = __ballot(set);
-            peers &= set ? with : ~with;
+    for (int e = 0; e < kPer; ++e) {
+        const int b = threadIdx.x * kPer + e;
+        if constexpr (SCANNED) {
+            before[e] = p.count[static_cast<int64_t>(blockIdx.x) * kBins + b];
+            total[e] = p.total[b];
+        } else {
+            before[e] = total[e] = 0;
         }
-        const int leader = there ? __ffsll(static_cast<unsigned long long>(peers)) - 1 : lane;
-        uint32_t old = 0;
-        if (there && lane == leader) old = atomicAdd(&seen[wave][digit], static_cast<uint32_t>(__popcll(peers)));
-        old = __shfl(old, leader);
-        rank[r] = old + static_cast<uint32_t>(__popcll(peers & ((1ull << lane) - 1)));
+    }
+    if constexpr (!SCANNED) {
+#pragma unroll 8
+        for (int t = 0; t < p.tiles; ++t) {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                const uint32_t c = p.count[static_cast<int64_t>(t) * kBins + threadIdx.x * kPer + e];
+                total[e] += c;
+                before[e] += t < static_cast<int>(blockIdx.x) ? c : 0u;
+            }
+        }
     }
     __syncthreads();
-    // thread t holds digit t: where its keys of each wave begin
-    {
-        const uint32_t mine = p.total[threadIdx.x];
-        uint32_t incl = mine;
 #pragma unroll
-        for (int off = 1; off < kWave; off <<= 1) {
-            const uint32_t o = __shfl_up(incl, off);
-            if (lane >= off) incl += o;
-        }
-        if (lane == 63) part[wave] = incl;
-        __syncthreads();
-        uint32_t start = incl - mine + p.count[static_cast<int64_t>(threadIdx.x) * p.tiles + blockIdx.x];
+    for (int r = 0; r < kPerThread; ++r) rank[r] = wave_rank(seen[wave], (key[r] >> p.shift) & mask, p.bits, first + r * kWave < p.n, lane);
+    __syncthreads();
+    uint32_t mine = 0;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w)
-            if (w < wave) start += part[w];
+    for (int e = 0; e < kPer; ++e) mine += total[e];
+    uint32_t at = block_scan<kThreads>(mine, part);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        uint32_t start = at + before[e];
+        at += total[e];
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            const uint32_t c = seen[w][threadIdx.x];
-            seen[w][threadIdx.x] = start;
+            const uint32_t c = seen[w][threadIdx.x * kPer + e];
+            seen[w][threadIdx.x * kPer + e] = start;
             start += c;
         }
     }
@@ -222,39 +327,61 @@ __global__ __launch_bounds__(kThreads) void sort_scatter_kernel(const SortArgs p
     for (int r = 0; r < kPerThread; ++r) {
         const int64_t i = first + r * kWave;
         if (i >= p.n) continue;
-        const uint32_t to = seen[wave][(key[r] >> p.shift) & ((1u << p.bits) - 1)] + rank[r];
+        const uint32_t to = seen[wave][(key[r] >> p.shift) & mask] + rank[r];
         p.key_out[to] = key[r];
         p.pos_out[to] = FIRST ? static_cast<uint32_t>(i) : p.pos_in[i];
     }
 }
 
-struct SortPlan {
+// ---- grad_table[v] = scale * the sum of the rows of id v -----------------------------------------------------
+// The sorted positions are cut into chunks of equal length, whatever the ids, so that a token that makes up a tenth of the batch
+// costs no more than others.  A chunk's rows are added up id by id; a sum that began and ended inside the chunk is a
+// finished row, one that reaches over its border goes to the workspace (slot 0 of the chunk: it began before; slot 1: it goes on), and
+// embed_join_kernel adds those up chunk by chunk.  Bound by HBM: the rows of grad_out read once, grad_table written once.
+constexpr int chunk_of(int64_t n) { return n <= 4096 ? 8 : (n <= 16384 ? 16 : (n <= 262144 ? 32 : 64)); }     // enough chunks for the chip, few partial sums
+
+struct EmbedGradPlan {
+    bool small;
     int passes, bits;
-    int64_t tiles;
-    size_t key0, pos0, key1, pos1, count, total, bytes;     // offsets in the workspace
+    int64_t tiles, chunks;
+    int chunk;
+    int64_t ld_part;
+    size_t key0, pos0, key1, pos1, count, total, part, bytes;     // offsets in the workspace
 };
 
-SortPlan plan_sort(int64_t n, int64_t table_rows)
+EmbedGradPlan plan_embed_grad(int64_t n, int64_t table_rows, int32_t dim)
 {
-    SortPlan s;
+    EmbedGradPlan s;
     const int bits = ceil_log2(table_rows + 1) < 1 ? 1 : ceil_log2(table_rows + 1);
-    s.passes = static_cast<int>(ceil_div(bits, kDigitBits));
+    s.small = n <= kSmall;
+    s.passes = static_cast<int>(ceil_div(bits, s.small ? kSmallBits : kDigitBits));
     s.bits = static_cast<int>(ceil_div(bits, s.passes));
     s.tiles = ceil_div(n, kTile);
+    s.chunk = chunk_of(n);
+    s.chunks = ceil_div(n, s.chunk);
+    s.ld_part = static_cast<int64_t>(round_up(static_cast<size_t>(dim), 8));
     const size_t list = round_up(static_cast<size_t>(n) * 4, 256);
-    s.key0 = 0; s.pos0 = list; s.key1 = 2 * list; s.pos1 = 3 * list; s.count = 4 * list;
-    s.total = s.count + round_up(static_cast<size_t>(s.tiles) * kBins * 4, 256);
-    s.bytes = s.total + kBins * 4;
+    s.key0 = 0; s.pos0 = list; s.key1 = 2 * list; s.pos1 = 3 * list;
+    s.count = s.small ? 2 * list : 4 * list;
+    s.total = s.count + (s.small ? 0 : static_cast<size_t>(s.tiles) * kBins * 4);
+    s.part = s.total + (s.small ? 0 : kBins * 4);
+    s.bytes = s.part + static_cast<size_t>(s.chunks) * 2 * s.ld_part * 4 + 256;
     return s;
 }
 
 template <typename Id>
-hipError_t sort_ids(const SortPlan &s, int64_t n, const void *ids, int64_t table_rows, char *ws, const uint32_t **keys, const uint32_t **pos, hipStream_t stream)
+hipError_t sort_ids(const EmbedGradPlan &s, int64_t n, const void *ids, int64_t table_rows, char *ws, const uint32_t **keys, const uint32_t **pos, hipStream_t stream)
 {
     uint32_t *key[2] = {reinterpret_cast<uint32_t *>(ws + s.key0), reinterpret_cast<uint32_t *>(ws + s.key1)};
     uint32_t *at[2] = {reinterpret_cast<uint32_t *>(ws + s.pos0), reinterpret_cast<uint32_t *>(ws + s.pos1)};
     SortArgs p{};
-    p.ids = ids; p.n = n; p.table_rows = table_rows; p.tiles = static_cast<int32_t>(s.tiles); p.bits = s.bits;
+    p.ids = ids; p.n = n; p.table_rows = table_rows; p.tiles = static_cast<int32_t>(s.tiles); p.bits = s.bits; p.passes = s.passes;
+    if (s.small) {
+        p.key_out = key[0]; p.pos_out = at[0];
+        *keys = key[0]; *pos = at[0];
+        hipLaunchKernelGGL((sort_small_kernel<Id>), dim3(1), dim3(kSmallThreads), 0, stream, p);
+        return hipGetLastError();
+    }
     p.count = reinterpret_cast<uint32_t *>(ws + s.count);
     p.total = reinterpret_cast<uint32_t *>(ws + s.total);
     const dim3 grid(static_cast<unsigned>(s.tiles)), block(kThreads);
@@ -264,9 +391,14 @@ hipError_t sort_ids(const SortPlan &s, int64_t n, const void *ids, int64_t table
         p.key_out = key[pass & 1]; p.pos_out = at[pass & 1];
         if (pass == 0) hipLaunchKernelGGL((sort_count_kernel<Id, true>), grid, block, 0, stream, p);
         else hipLaunchKernelGGL((sort_count_kernel<Id, false>), grid, block, 0, stream, p);
-        hipLaunchKernelGGL(sort_scan_kernel, dim3(kBins), block, 0, stream, p);
-        if (pass == 0) hipLaunchKernelGGL((sort_scatter_kernel<Id, true>), grid, block, 0, stream, p);
-        else hipLaunchKernelGGL((sort_scatter_kernel<Id, false>), grid, block, 0, stream, p);
+        if (s.tiles > kScanTiles) {
+            hipLaunchKernelGGL(sort_scan_kernel, dim3(kBins / kWave), block, 0, stream, p);
+            if (pass == 0) hipLaunchKernelGGL((sort_scatter_kernel<Id, true, true>), grid, block, 0, stream, p);
+            else hipLaunchKernelGGL((sort_scatter_kernel<Id, false, true>), grid, block, 0, stream, p);
+        } else {
+            if (pass == 0) hipLaunchKernelGGL((sort_scatter_kernel<Id, true, false>), grid, block, 0, stream, p);
+            else hipLaunchKernelGGL((sort_scatter_kernel<Id, false, false>), grid, block, 0, stream, p);
+        }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -275,72 +407,194 @@ hipError_t sort_ids(const SortPlan &s, int64_t n, const void *ids, int64_t table
     return hipSuccess;
 }
 
-// ---- grad_table[v] = scale * the sum of the rows of id v -----------------------------------------------------
 template <typename In, typename Out>
 struct SumArgs {
     const uint32_t *keys, *pos;
     const In *grad;
     Out *out;
-    int64_t n, table_rows, ld_grad, ld_out;
-    int32_t dim;
+    float *part;
+    int64_t n, table_rows, ld_grad, ld_out, ld_part, sum_blocks;
+    int32_t dim, chunk, chunks, lanes_log2, slabs;
     float scale;
     int32_t accumulate;
 };
 
-__device__ __forceinline__ int64_t lower_bound(const uint32_t *a, int64_t n, uint32_t v)
+// the first place in sorted a[lo, hi) whose key is not below v, by a wavefront: 64 places at a time, so that a list of 2^18 takes three loads one after the other
+__device__ __forceinline__ int64_t wave_lower_bound(const uint32_t *a, int64_t lo, int64_t hi, uint32_t v, int lane)
 {
-    int64_t lo = 0;
-    while (n > 0) {
-        const int64_t half = n >> 1;
-        if (a[lo + half] < v) { lo += half + 1; n -= half + 1; }
-        else n = half;
+    while (hi - lo > kWave) {
+        const int64_t step = (hi - lo + kWave - 1) / kWave, at = lo + lane * step;
+        const int below = __popcll(__ballot(at < hi && a[at] < v));
+        if (below == 0) return lo;
+        hi = lo + below * step < hi ? lo + below * step : hi;
+        lo += (below - 1) * step + 1;
     }
-    return lo;
+    return lo + __popcll(__ballot(lo + lane < hi && a[lo + lane] < v));
 }
 
-// a wavefront per table row and slab of 64 * VEC columns
+// which of the 64 ids from `first` on the sorted list has: a bit each.  A step passes 64 keys, or all of the last one's kind.
+__device__ __forceinline__ uint64_t ids_present(const uint32_t *keys, int64_t n, uint32_t first, int lane)
+{
+    uint64_t present = 0;
+    int64_t at = wave_lower_bound(keys, 0, n, first, lane);
+    while (at < n) {
+        const uint32_t key = at + lane < n ? keys[at + lane] : 0xffffffffu;
+        const bool mine = key - first < kWave;
+        uint64_t bit = mine ? 1ull << (key - first) : 0ull;
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) bit |= __shfl_xor(bit, off);
+        present |= bit;
+        const uint32_t last = __builtin_amdgcn_readlane(key, 63);
+        if (last - first >= kWave) break;
+        at = wave_lower_bound(keys, at + kWave, n, last + 1, lane);
+    }
+    return present;
+}
+
+// columns [c, c + VEC) of a finished row; with the last vector moved back to `col` the columns before c are the neighbour's
+template <typename In, typename Out, int VEC>
+__device__ __forceinline__ void put_row(const SumArgs<In, Out> &p, uint32_t row, int c, int col, const float (&sum)[VEC])
+{
+    Out *o = p.out + static_cast<int64_t>(row) * p.ld_out;
+    float v[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[e] = p.scale * sum[e];
+    if (c == col) {
+        if (p.accumulate) {
+            float old[VEC];
+            load_n<VEC>(o + c, old);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) v[e] += old[e];
+        }
+        store_n<VEC>(o + c, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (col + e >= c) from_f32(v[e] + (p.accumulate ? to_f32(o[col + e]) : 0.f), o[col + e]);
+    }
+}
+
+// Blocks up to sum_blocks: 2^lanes_log2 lanes per chunk (and slab of columns).  The others write zeros to the rows that no id names.
 template <typename In, typename Out, int VEC>
 __global__ __launch_bounds__(kThreads) void embed_sum_kernel(const SumArgs<In, Out> p)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t v = static_cast<int64_t>(blockIdx.x) * (kThreads / kWave) + (threadIdx.x >> 6);
-    if (v >= p.table_rows) return;
-    const int64_t beg = lower_bound(p.keys, p.n, static_cast<uint32_t>(v)), end = beg + lower_bound(p.keys + beg, p.n - beg, static_cast<uint32_t>(v + 1));
-    if (beg == end && p.accumulate) return;
-    for (int64_t c = (static_cast<int64_t>(blockIdx.y) * kWave + lane) * VEC; c < p.dim; c += static_cast<int64_t>(gridDim.y) * kWave * VEC) {
-        float sum[VEC];
+    const int lanes = 1 << p.lanes_log2;
+    if (static_cast<int64_t>(blockIdx.x) >= p.sum_blocks) {
+        const int lane = threadIdx.x & 63;
+        const int64_t row0 = ((static_cast<int64_t>(blockIdx.x) - p.sum_blocks) * (kThreads / kWave) + (threadIdx.x >> 6)) * kWave;
+        if (row0 >= p.table_rows) return;
+        const int64_t left = p.table_rows - row0;
+        const uint64_t rows = ~ids_present(p.keys, p.n, static_cast<uint32_t>(row0), lane) & (left < kWave ? (1ull << left) - 1 : ~0ull);
+        constexpr int VO = VEC == 1 ? 1 : 16 / static_cast<int>(sizeof(Out));
+        const float zero[VO] = {};
+        for (int r = lane >> p.lanes_log2; r < kWave; r += kWave >> p.lanes_log2)
+            if ((rows >> r) & 1)
+                for (int c = (lane & (lanes - 1)) * VO; c < p.dim; c += lanes * VO)
+                    store_n<VO>(p.out + (row0 + r) * p.ld_out + (c + VO <= p.dim ? c : p.dim - VO), zero);
+        return;
+    }
+    constexpr int U = 8;
+    const int64_t group = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) >> p.lanes_log2;
+    const int64_t chunk = group / p.slabs;
+    const int c = static_cast<int>(((group % p.slabs) << p.lanes_log2) + (threadIdx.x & (lanes - 1))) * VEC;
+    if (chunk >= p.chunks || c >= p.dim) return;
+    const int col = c + VEC <= p.dim ? c : p.dim - VEC;
+    const int64_t beg = chunk * p.chunk, end = beg + p.chunk < p.n ? beg + p.chunk : p.n;
+    const uint32_t none = static_cast<uint32_t>(p.table_rows);
+    uint32_t cur = p.keys[beg];
+    bool head = beg > 0 && p.keys[beg - 1] == cur;
+    float sum[VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sum[e] = 0.f;
-        const bool whole = c + VEC <= p.dim;
-        for (int64_t i = beg; i < end; ++i) {
-            const In *g = p.grad + static_cast<int64_t>(p.pos[i]) * p.ld_grad + c;
-            if (whole) {
-                float x[VEC];
-                load_n<VEC>(g, x);
+    for (int e = 0; e < VEC; ++e) sum[e] = 0.f;
+    auto finish = [&](bool tail) {
+        if (cur != none) {
+            if (head || tail) store_n<VEC>(p.part + (2 * chunk + (head ? 0 : 1)) * p.ld_part + c, sum);
+            else put_row<In, Out, VEC>(p, cur, c, col, sum);
+        }
+        head = false;
+    };
+    for (int64_t i = beg; i < end; i += U) {
+        uint32_t key[U], pos[U];
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) sum[e] += x[e];
+        for (int u = 0; u < U; ++u) {
+            key[u] = i + u < end ? p.keys[i + u] : none;
+            pos[u] = i + u < end ? p.pos[i + u] : 0u;
+        }
+        float x[U][VEC];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (key[u] != none) {
+                load_n<VEC>(p.grad + static_cast<int64_t>(pos[u]) * p.ld_grad + col, x[u]);
             } else {
 #pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    if (c + e < p.dim) sum[e] += to_f32(g[e]);
+                for (int e = 0; e < VEC; ++e) x[u][e] = 0.f;
             }
         }
-        Out *o = p.out + v * p.ld_out + c;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            if (c + e < p.dim) from_f32((p.accumulate ? to_f32(o[e]) : 0.f) + p.scale * sum[e], o[e]);
+        for (int u = 0; u < U; ++u) {
+            if (i + u < end && key[u] != cur) {
+                finish(false);
+                cur = key[u];
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) sum[e] = 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sum[e] += x[u][e];
+        }
     }
+    finish(end < p.n && p.keys[end] == cur);
 }
 
-template <typename In, typename Out>
-hipError_t embed_sum(const uint32_t *keys, const uint32_t *pos, int64_t n, int64_t table_rows, const void *grad, int32_t dim, int64_t ld_grad, float scale,
-                     bool accumulate, void *out, int64_t ld_out, hipStream_t stream)
+// The sums that reach over a chunk's end: a block per chunk and slab in which one begins.  Its groups of lanes add up equal shares of
+// the partial sums, which then meet in LDS, in order.
+template <typename In, typename Out, int VEC>
+__global__ __launch_bounds__(kThreads) void embed_join_kernel(const SumArgs<In, Out> p)
 {
-    constexpr int VEC = 4;
-    const SumArgs<In, Out> p{keys, pos, static_cast<const In *>(grad), static_cast<Out *>(out), n, table_rows, ld_grad, ld_out, dim, scale, accumulate};
-    const int64_t slabs = ceil_div(dim, kWave * VEC);
-    hipLaunchKernelGGL((embed_sum_kernel<In, Out, VEC>), dim3(static_cast<unsigned>(ceil_div(table_rows, kThreads / kWave)), static_cast<unsigned>(slabs < 1024 ? slabs : 1024)),
-                       dim3(kThreads), 0, stream, p);
+    __shared__ float joined[kThreads * VEC];
+    const int64_t chunk = blockIdx.x / p.slabs, beg = chunk * p.chunk, end = beg + p.chunk;
+    if (end >= p.n) return;
+    const uint32_t id = p.keys[end - 1];
+    if (id != p.keys[end] || id == static_cast<uint32_t>(p.table_rows)) return;
+    if (p.keys[beg] == id && beg > 0 && p.keys[beg - 1] == id) return;              // it began in an earlier one
+    const int64_t last = (wave_lower_bound(p.keys, end, p.n, id + 1, threadIdx.x & 63) - 1) / p.chunk;
+    const int lanes = 1 << p.lanes_log2, groups = kThreads >> p.lanes_log2, group = threadIdx.x >> p.lanes_log2;
+    const int c = static_cast<int>(((blockIdx.x % p.slabs) << p.lanes_log2) + (threadIdx.x & (lanes - 1))) * VEC;
+    const int64_t count = last - chunk + 1, share = (count + groups - 1) / groups, from = group * share, to = from + share < count ? from + share : count;
+    float sum[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) sum[e] = 0.f;
+    if (c < p.dim) {
+#pragma unroll 8
+        for (int64_t i = from; i < to; ++i) {
+            float x[VEC];
+            load_n<VEC>(p.part + (2 * (chunk + i) + (i == 0 ? 1 : 0)) * p.ld_part + c, x);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sum[e] += x[e];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) joined[e * kThreads + threadIdx.x] = sum[e];
+    __syncthreads();
+    if (group != 0 || c >= p.dim) return;
+    for (int g = 1; g < groups && g * share < count; ++g) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sum[e] += joined[e * kThreads + (g << p.lanes_log2) + threadIdx.x];
+    }
+    put_row<In, Out, VEC>(p, id, c, c + VEC <= p.dim ? c : p.dim - VEC, sum);
+}
+
+template <typename In, typename Out, int VEC>
+hipError_t embed_sum(const EmbedGradPlan &s, SumArgs<In, Out> p, hipStream_t stream)
+{
+    const int64_t vecs = ceil_div(p.dim, VEC);
+    p.lanes_log2 = ceil_log2(vecs) < 6 ? ceil_log2(vecs) : 6;
+    p.slabs = static_cast<int32_t>(ceil_div(vecs, static_cast<int64_t>(1) << p.lanes_log2));
+    p.sum_blocks = ceil_div((s.chunks * p.slabs) << p.lanes_log2, kThreads);
+    const int64_t fill_blocks = p.accumulate ? 0 : ceil_div(p.table_rows, kThreads);
+    if (p.sum_blocks + fill_blocks > INT32_MAX || s.chunks * p.slabs > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (p.sum_blocks + fill_blocks == 0) return hipSuccess;
+    hipLaunchKernelGGL((embed_sum_kernel<In, Out, VEC>), dim3(static_cast<unsigned>(p.sum_blocks + fill_blocks)), dim3(kThreads), 0, stream, p);
+    if (s.chunks > 1) hipLaunchKernelGGL((embed_join_kernel<In, Out, VEC>), dim3(static_cast<unsigned>(s.chunks * p.slabs)), dim3(kThreads), 0, stream, p);
     return hipGetLastError();
 }
 
@@ -360,21 +614,27 @@ mgg_status_t launch_embed(int64_t n, mgg_index_t id_type, const void *ids, int64
     return e == hipSuccess ? MGG_OK : hip_fail(e, "lookup kernel launch");
 }
 
-size_t embed_grad_workspace(int64_t n, int64_t table_rows, int32_t dim) { return round_up(plan_sort(n, table_rows).bytes, 256); }
+size_t embed_grad_workspace(int64_t n, int64_t table_rows, int32_t dim) { return plan_embed_grad(n, table_rows, dim).bytes; }
 
 mgg_status_t launch_embed_grad(int64_t n, mgg_index_t id_type, const void *ids, int64_t table_rows, mgg_dtype_t grad_dtype, const void *grad, int32_t dim,
                                int64_t ld_grad, float scale, bool accumulate, mgg_dtype_t out_dtype, void *out, int64_t ld_out, void *workspace,
                                hipStream_t stream)
 {
-    const SortPlan s = plan_sort(n, table_rows);
+    const EmbedGradPlan s = plan_embed_grad(n, table_rows, dim);
+    char *ws = static_cast<char *>(workspace);
     const uint32_t *keys = nullptr, *pos = nullptr;
     hipError_t e = hipSuccess;
     if (n > 0) {
-        e = id_type == MGG_I64 ? sort_ids<int64_t>(s, n, ids, table_rows, static_cast<char *>(workspace), &keys, &pos, stream)
-                               : sort_ids<int32_t>(s, n, ids, table_rows, static_cast<char *>(workspace), &keys, &pos, stream);
+        e = id_type == MGG_I64 ? sort_ids<int64_t>(s, n, ids, table_rows, ws, &keys, &pos, stream) : sort_ids<int32_t>(s, n, ids, table_rows, ws, &keys, &pos, stream);
         if (e != hipSuccess) return hip_fail(e, "sort kernel launch");
     }
-#define MGG_SUM(IN, OUT) e = embed_sum<IN, OUT>(keys, pos, n, table_rows, grad, dim, ld_grad, scale, accumulate, out, ld_out, stream)
+#define MGG_SUM(IN, OUT)                                                                                                                                      \
+    do {                                                                                                                                                      \
+        const SumArgs<IN, OUT> p{keys, pos, static_cast<const IN *>(grad), static_cast<OUT *>(out), reinterpret_cast<float *>(ws + s.part), n, table_rows,       \
+                                 ld_grad, ld_out, s.ld_part, 0, dim, s.chunk, static_cast<int32_t>(s.chunks), 0, 0, scale, accumulate};                         \
+        constexpr int VEC = 16 / sizeof(IN);                                                                                                                  \
+        e = dim < 8 ? embed_sum<IN, OUT, 1>(s, p, stream) : embed_sum<IN, OUT, VEC>(s, p, stream);                                                              \
+    } while (0)
     if (grad_dtype == MGG_BF16) { if (out_dtype == MGG_BF16) MGG_SUM(Bf16, Bf16); else MGG_SUM(Bf16, float); }
     else { if (out_dtype == MGG_BF16) MGG_SUM(float, Bf16); else MGG_SUM(float, float); }
 #undef MGG_SUM
