@@ -21,11 +21,11 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 struct Vec16 { uint32_t u[4]; };
 
-// ---- which rows a block has ----------------------------------------------------------------------------------
-struct Span { int32_t group, row, end, index, total; };     // rows [row, end) of the group: piece `index` of `total` in all
+constexpr int kBandRows = 1024;     // rows of a band of tiles
 
-// The groups cut every `step` rows: piece number `index`, found by every wavefront for itself (64 groups at a time, a group per
-// lane).  With xcds > 1 `index` counts through pieces dealt in contiguous runs to the XCDs (block b runs on XCD b mod 8).
+// ---- which rows a block has ----------------------------------------------------------------------------------
+struct Span { int32_t group, row, end; };       // rows [row, end) of the group
+
 __device__ __forceinline__ void group_range(const int64_t *ptr, int g, int n_groups, int64_t n_rows, int32_t *lo, int32_t *hi)
 {
     *lo = *hi = 0;
@@ -45,7 +45,23 @@ __device__ __forceinline__ int wave_scan(int v, int lane)
     return v;
 }
 
+__device__ __forceinline__ int pieces_in(int32_t rows, int step) { return rows / step + (rows % step != 0); }
 
+// pieces of `step` rows in the first n_groups groups, by a wavefront, a group per lane; `most` where overlapping groups would give more
+__device__ __forceinline__ int count_pieces(const int64_t *ptr, int n_groups, int64_t n_rows, int step, int most)
+{
+    int count = 0;
+    for (int g = threadIdx.x & 63; g < n_groups; g += kWave) {
+        int32_t lo, hi;
+        group_range(ptr, g, n_groups, n_rows, &lo, &hi);
+        count = min(count + pieces_in(hi - lo, step), most);
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) count = min(count + __shfl_xor(count, off), most);
+    return __builtin_amdgcn_readfirstlane(count);
+}
+
+// piece number `index`, found by every wavefront for itself, 64 groups at a time
 __device__ __forceinline__ bool find_piece(const int64_t *ptr, int n_groups, int64_t n_rows, int step, int index, Span *s)
 {
     const int lane = threadIdx.x & 63;
@@ -53,21 +69,28 @@ __device__ __forceinline__ bool find_piece(const int64_t *ptr, int n_groups, int
     for (int g0 = 0; g0 < n_groups; g0 += kWave) {
         int32_t lo, hi;
         group_range(ptr, g0 + lane, n_groups, n_rows, &lo, &hi);
-        const int count = (hi - lo) / step + ((hi - lo) % step != 0);
+        const int count = pieces_in(hi - lo, step);
         const int incl = wave_scan(count, lane);
         const uint64_t past = __ballot(before + incl > index);
         if (past) {
             const int at = __ffsll(static_cast<unsigned long long>(past)) - 1;
-            s->group = g0 + at;
             const int first = __shfl(lo, at) + (index - before - __shfl(incl - count, at)) * step, last = __shfl(hi, at);
+            s->group = g0 + __builtin_amdgcn_readfirstlane(at);
             s->row = __builtin_amdgcn_readfirstlane(first);
             s->end = __builtin_amdgcn_readfirstlane(last - first < step ? last : first + step);
-            s->group = __builtin_amdgcn_readfirstlane(s->group);
             return true;
         }
         before += __shfl(incl, 63);
     }
     return false;
+}
+
+// tile number `index` of rows x cols, in bands of `band` rows, each walked column by column
+__device__ __forceinline__ void band_order(int index, int rows, int cols, int band, int *row, int *col)
+{
+    const int b = index / (band * cols), in = index % (band * cols), high = rows - b * band < band ? rows - b * band : band;
+    *col = in / high;
+    *row = b * band + in % high;
 }
 
 // ---- an operand's tile on its way from memory to the matrix cores ----------------------------------------------
@@ -83,37 +106,29 @@ __device__ __forceinline__ Vec16 load16(const T *p)
     return v;
 }
 
-// the first `have` elements at p, zeros behind them; reads nothing outside a row of `len` elements that begins at `row`
+// the elements of v from number `skip` (0 .. N) on, zeros behind them
 template <typename T>
-__device__ __forceinline__ Vec16 load16_edge(const T *row, int64_t at, int have, int64_t len)
+__device__ __forceinline__ Vec16 drop(const Vec16 &v, int skip)
 {
-    constexpr int N = Elem<T>::N;
-    Vec16 v{{0u, 0u, 0u, 0u}};
-    if (have >= N) return load16(row + at);
-    if (have <= 0) return v;
-    if (len >= N) {
-        // ends with the row: what lies before `at` is shifted out
-        const Vec16 w = load16(row + at + have - N);
-        const int bits = (N - have) * static_cast<int>(sizeof(T)) * 8, dwords = bits >> 5, rest = bits & 31;
-        uint32_t u[5] = {w.u[0], w.u[1], w.u[2], w.u[3], 0u};
-        if (dwords & 1) { u[0] = u[1]; u[1] = u[2]; u[2] = u[3]; u[3] = 0u; }
-        if (dwords & 2) { u[0] = u[2]; u[1] = u[3]; u[2] = 0u; u[3] = 0u; }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v.u[i] = __builtin_amdgcn_alignbit(i < 3 ? u[i + 1] : 0u, u[i], rest);
-        return v;
-    }
-    T e[N];
-    __builtin_memset(e, 0, sizeof e);
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        if (i < have) e[i] = row[at + i];
-    __builtin_memcpy(&v, e, 16);
-    return v;
+    const int bits = skip * static_cast<int>(sizeof(T)) * 8;
+    const bool one = bits & 32, two = bits & 64, all = bits & 128;
+    const uint32_t a0 = one ? v.u[1] : v.u[0], a1 = one ? v.u[2] : v.u[1], a2 = one ? v.u[3] : v.u[2], a3 = one ? 0u : v.u[3];
+    const uint32_t b0 = two ? a2 : a0, b1 = two ? a3 : a1, b2 = two ? 0u : a2, b3 = two ? 0u : a3;
+    const uint32_t rest = bits & 31;
+    Vec16 r;
+    r.u[0] = all ? 0u : __builtin_amdgcn_alignbit(b1, b0, rest);
+    r.u[1] = all ? 0u : __builtin_amdgcn_alignbit(b2, b1, rest);
+    r.u[2] = all ? 0u : __builtin_amdgcn_alignbit(b3, b2, rest);
+    r.u[3] = all ? 0u : b3 >> rest;
+    return r;
 }
 
 // ALONG: rows of the tile are rows of the matrix, the sum runs along them.  Else the sum runs over the matrix's rows and the tile's
-// R rows are R of its columns.
-template <typename T, int R, bool ALONG, int THREADS>
+// R rows are R of its columns.  ODD: rows need not be whole chunks of 16 bytes (they have one at least).
+// Nothing outside the matrix is read: rows and columns that are not there are read from the nearest ones that are, 16 bytes that would
+// reach over a row's end from so far before it that they end with the row, and shifted.  What that leaves in places of the sum that do not exist
+// is zeroed, what it leaves in rows or columns of the result that do not exist is never written.
+template <typename T, int R, bool ALONG, int THREADS, bool ODD>
 struct Operand {
     static constexpr int N = Elem<T>::N, BK = Elem<T>::BK;
     static constexpr int kBytes = R * 128;
@@ -121,46 +136,86 @@ struct Operand {
     static constexpr int kRowChunks = ALONG ? 8 : R / N;        // 16-byte chunks per row in LDS
     static_assert(kPer * THREADS * 16 == kBytes, "a tile is whole chunks of every thread");
 
-    const T *base;      // ALONG: first row of the tile; else first row of the sum
+    const T *base;      // ALONG: first row of the tile; else first row of the sum (column 0 of the matrix)
     int64_t ld;
     int32_t rows;       // ALONG: rows of the tile that exist; else columns of the matrix from the tile's first on
     int32_t col0;       // else: the tile's first column
     int32_t depth;      // length of the sum
-    Vec16 v[kPer];
+    uint32_t off[kPer]; // bytes from `base`
+    Vec16 v[kPer];      // a step on its way
 
-    // chunk c of row r lies where neighbouring rows' chunks of one column meet different banks
+    // Chunk c of row r lies where what is read at once meets different banks: along, 16 lanes read a chunk of 16 rows (256 bytes, all
+    // banks); across, 32 lanes read 64 bytes of 4 rows (bf16) or 64 lanes 128 bytes of 2 rows, 4 apart (fp32).
     static __device__ __forceinline__ int place(int r, int c)
     {
-        if constexpr (ALONG) return r * 128 + ((c ^ (r & 7)) << 4);
+        if constexpr (ALONG) return r * 128 + ((c ^ ((r >> 1) & 7)) << 4);
         else {
             constexpr int G = sizeof(T) == 2 ? 4 : 8;            // chunks of 32 columns
-            constexpr int M = R / 32 < 4 ? R / 32 - 1 : 3;
-            const int key = (sizeof(T) == 2 ? r : r >> 2) & M;
+            const int key = sizeof(T) == 4 ? (r >> 2) & 1 : (R >= 128 ? r & 3 : (r >> 1) & 1);
             return r * R * static_cast<int>(sizeof(T)) + ((((c / G) ^ key) * G + c % G) << 4);
         }
     }
-    __device__ __forceinline__ void load(int k0)
+    static __device__ __forceinline__ int chunk_row(int i) { return (threadIdx.x % THREADS + i * THREADS) / kRowChunks; }
+    static __device__ __forceinline__ int chunk_col(int i) { return (threadIdx.x % THREADS + i * THREADS) % kRowChunks; }
+    // place of this thread's chunk i: where all of them have the same key, one address and constants
+    static __device__ __forceinline__ int chunk_place(int i)
+    {
+        constexpr int kStep = THREADS / kRowChunks;
+        if constexpr (kStep % (ALONG ? 16 : 8) == 0) return place(chunk_row(0), chunk_col(0)) + i * kStep * (ALONG ? 128 : R * static_cast<int>(sizeof(T)));
+        else return place(chunk_row(i), chunk_col(i));
+    }
+    // (32 bits hold an offset: at most 256 rows of 2^22 elements of 4 bytes)
+    __device__ __forceinline__ void init()
     {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int id = threadIdx.x + i * THREADS, r = id / kRowChunks, c = id % kRowChunks;
-            if constexpr (ALONG) {
-                const T *row = base + static_cast<int64_t>(r < rows ? r : rows - 1) * ld;
-                v[i] = load16_edge(row, k0 + c * N, depth - k0 - c * N, depth);
+            const int r = ALONG ? min(chunk_row(i), rows - 1) : chunk_row(i), c = ALONG ? chunk_col(i) * N : min(col0 + chunk_col(i) * N, col0 + rows - N);
+            off[i] = (static_cast<uint32_t>(r) * static_cast<uint32_t>(ld) + static_cast<uint32_t>(c)) * static_cast<uint32_t>(sizeof(T));
+        }
+    }
+    __device__ __forceinline__ const char *step_base(int k0) const
+    {
+        return reinterpret_cast<const char *>(base) + (ALONG ? static_cast<int64_t>(k0) : static_cast<int64_t>(k0) * ld) * static_cast<int64_t>(sizeof(T));
+    }
+    // a step whose BK places of the sum all exist
+    __device__ __forceinline__ void load_chunk(const char *at, int i) { v[i] = load16(reinterpret_cast<const T *>(at + off[i])); }
+    // the last one, where they do not
+    __device__ __forceinline__ void load_last(int k0)
+    {
+        const char *at = step_base(k0);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int over = ALONG ? max(k0 + chunk_col(i) * N + N - depth, 0) : max(k0 + chunk_row(i) - (depth - 1), 0);
+            const Vec16 x = load16(reinterpret_cast<const T *>(at + off[i]) - (ALONG ? over : over * ld));
+            if (ALONG && ODD) {
+                v[i] = drop<T>(x, min(over, N));
             } else {
-                const bool there = k0 + r < depth;
-                const T *row = base + static_cast<int64_t>(there ? k0 + r : 0) * ld;
-                v[i] = load16_edge(row, col0 + c * N, there ? rows - c * N : 0, static_cast<int64_t>(col0) + rows);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[i].u[e] = over ? 0u : x.u[e];
             }
         }
+    }
+    __device__ __forceinline__ void load(int t)
+    {
+        const int k0 = t * BK;
+        if (k0 + BK <= depth) {
+            const char *at = step_base(k0);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) load_chunk(at, i);
+        } else if (k0 < depth) {
+            load_last(k0);
+        }
+    }
+    __device__ __forceinline__ void store_chunk(char *lds, int i) const
+    {
+        Vec16 x = v[i];
+        if (ODD && !ALONG && rows < R) x = drop<T>(x, min(max(chunk_col(i) * N + N - rows, 0), N));
+        __builtin_memcpy(__builtin_assume_aligned(lds + chunk_place(i), 16), &x, 16);
     }
     __device__ __forceinline__ void store(char *lds) const
     {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int id = threadIdx.x + i * THREADS;
-            __builtin_memcpy(__builtin_assume_aligned(lds + place(id / kRowChunks, id % kRowChunks), 16), &v[i], 16);
-        }
+        for (int i = 0; i < kPer; ++i) store_chunk(lds, i);
     }
     // step s of the tile's depth (32 bytes of it) for the 32 rows from r0 on: lane (i, h) gets row r0 + i and, bf16, elements
     // 16 s + 8 h .. + 7, fp32, elements 8 s + 4 h .. + 3
@@ -214,91 +269,259 @@ struct Sink {
 };
 
 template <typename Out>
-__device__ __forceinline__ void put4(Out *o, float (&v)[4], int cols, bool add)
+__device__ __forceinline__ void put8(Out *o, float (&v)[8], int cols, bool add)
 {
-    if (cols >= 4) {
+    if (cols >= 8) {
         if (add) {
-            float old[4];
-            load_n<4>(o, old);
+            float old[8];
+            load_n<8>(o, old);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += old[e];
+            for (int e = 0; e < 8; ++e) v[e] += old[e];
         }
-        store_n<4>(o, v);
+        store_n<8>(o, v);
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+        for (int e = 0; e < 8; ++e)
             if (e < cols) from_f32(v[e] + (add ? to_f32(o[e]) : 0.f), o[e]);
     }
 }
 
+// The two halves of a wavefront change registers, so that a lane has eight neighbouring columns: 16 (q + h), q = 0, 1, of row m.
 __device__ __forceinline__ void put_tile(const Sink &p, const f32x16 &acc, int64_t row, int64_t end, int col0, int lane)
 {
     const int64_t r = row + (lane & 31);
-    if (r >= end) return;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int col = col0 + 8 * q + 4 * (lane >> 5);
-        if (col >= p.n_cols) continue;
-        float v[4];
+    for (int q = 0; q < 2; ++q) {
+        float v[8];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            v[e] = acc[4 * q + e] + (p.bias && col + e < p.n_cols ? p.bias[col + e] : 0.f);
-            if (p.relu) v[e] = v[e] > 0.f || v[e] != v[e] ? v[e] : 0.f;
+            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[8 * q + e]), __float_as_uint(acc[8 * q + 4 + e]), false, false);
+            v[e] = __uint_as_float(both[0]);
+            v[4 + e] = __uint_as_float(both[1]);
         }
-        if (p.bf16) put4(static_cast<Bf16 *>(p.out) + r * p.ld + col, v, p.n_cols - col, p.add);
-        else put4(static_cast<float *>(p.out) + r * p.ld + col, v, p.n_cols - col, p.add);
+        const int col = col0 + 16 * q + 8 * (lane >> 5);
+        if (r >= end || col >= p.n_cols) continue;
+        if (p.bias) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += p.bias[col + e < p.n_cols ? col + e : p.n_cols - 1];
+        }
+        if (p.relu) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = v[e] < 0.f ? 0.f : v[e];
+        }
+        if (p.bf16) put8(static_cast<Bf16 *>(p.out) + r * p.ld + col, v, p.n_cols - col, p.add);
+        else put8(static_cast<float *>(p.out) + r * p.ld + col, v, p.n_cols - col, p.add);
     }
 }
 
-template <typename T, int BM, int BN, int WM, int WN, bool A_ALONG, bool B_ALONG>
+// A tile of BM x BN of the result by THREADS threads: WM x WN wavefronts, TM x TN pieces of 32 x 32 each
+template <typename T, int BM, int BN, int WM, int WN, bool A_ALONG, bool B_ALONG, bool ODD>
 struct Tile {
-    static constexpr int THREADS = 64 * WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
-    using A = Operand<T, BM, A_ALONG, THREADS>;
-    using B = Operand<T, BN, B_ALONG, THREADS>;
-    static constexpr int kLds = A::kBytes + B::kBytes;
+    static constexpr int THREADS = 64 * WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, BK = Elem<T>::BK;
+    using A = Operand<T, BM, A_ALONG, THREADS, ODD>;
+    using B = Operand<T, BN, B_ALONG, THREADS, ODD>;
+    static constexpr int kStage = A::kBytes + B::kBytes;
+    typedef f32x16 Acc[TM][TN];
 
-    // acc = the product of the two operands' tiles over their whole depth
-    static __device__ __forceinline__ void run(A &a, B &b, char *lds, f32x16 (&acc)[TM][TN])
+    static __device__ __forceinline__ int wave_row() { return threadIdx.x % THREADS / 64 / WN * TM * 32; }
+    static __device__ __forceinline__ int wave_col() { return threadIdx.x % THREADS / 64 % WN * TN * 32; }
+    static __device__ __forceinline__ void clear(Acc &acc)
     {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-        constexpr int BK = Elem<T>::BK;
-        const int steps = (a.depth + BK - 1) / BK;
-        for (int t = 0; t < steps; ++t) {
-            a.load(t * BK);
-            b.load(t * BK);
-            __syncthreads();
-            a.store(lds);
-            b.store(lds + A::kBytes);
-            __syncthreads();
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                Vec16 fa[TM], fb[TN];
-#pragma unroll
-                for (int i = 0; i < TM; ++i) fa[i] = A::frag(lds, (wm * TM + i) * 32, s, lane);
-#pragma unroll
-                for (int j = 0; j < TN; ++j) fb[j] = B::frag(lds + A::kBytes, (wn * TN + j) * 32, s, lane);
-#pragma unroll
-                for (int i = 0; i < TM; ++i)
-#pragma unroll
-                    for (int j = 0; j < TN; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j]);
-            }
-        }
     }
-    static __device__ __forceinline__ void put(const Sink &p, const f32x16 (&acc)[TM][TN], int64_t row0, int64_t end, int col0)
+    // quarter s of a step out of LDS
+    static __device__ __forceinline__ void read(const char *lds, int s, Vec16 (&fa)[TM], Vec16 (&fb)[TN])
     {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) fb[j] = B::frag(lds + A::kBytes, wave_col() + j * 32, s, lane);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) fa[i] = A::frag(lds, wave_row() + i * 32, s, lane);
+    }
+    static __device__ __forceinline__ void multiply_quarter(const Vec16 (&fa)[TM], const Vec16 (&fb)[TN], Acc &acc)
+    {
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) put_tile(p, acc[i][j], row0 + (wm * TM + i) * 32, end, col0 + (wn * TN + j) * 32, lane);
+            for (int j = 0; j < TN; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j]);
+    }
+    static __device__ __forceinline__ void multiply_step(const char *lds, Acc &acc)
+    {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            Vec16 fa[TM], fb[TN];
+            read(lds, s, fa, fb);
+            multiply_quarter(fa, fb, acc);
+        }
+    }
+    static __device__ __forceinline__ void load(A &a, B &b, int t)
+    {
+        a.load(t);
+        b.load(t);
+    }
+    static __device__ __forceinline__ void load_plain(A &a, B &b, int t)
+    {
+        const char *at_a = a.step_base(t * BK), *at_b = b.step_base(t * BK);
+#pragma unroll
+        for (int i = 0; i < A::kPer; ++i) a.load_chunk(at_a, i);
+#pragma unroll
+        for (int i = 0; i < B::kPer; ++i) b.load_chunk(at_b, i);
+    }
+    static __device__ __forceinline__ void store(const A &a, const B &b, char *lds)
+    {
+        a.store(lds);
+        b.store(lds + A::kBytes);
+    }
+
+    // acc = the product of the two operands' tiles over their whole depth, by all threads of the block; lds: two stages.  While a
+    // step is multiplied out of one, the next one goes from registers to the other and the one after it is on its way from memory.
+    static __device__ __forceinline__ void run(A &a, B &b, char *lds, Acc &acc)
+    {
+        clear(acc);
+        const int steps = (a.depth + BK - 1) / BK;
+        if (steps == 0) return;
+        a.init();
+        b.init();
+        load(a, b, 0);
+        store(a, b, lds);
+        load(a, b, 1);
+        __syncthreads();
+        int t = 0;
+        for (; t + 2 < a.depth / BK; ++t) {
+            store(a, b, lds + ((t + 1) & 1) * kStage);
+            load_plain(a, b, t + 2);
+            multiply_step(lds + (t & 1) * kStage, acc);
+            __syncthreads();
+        }
+        for (; t + 1 < steps; ++t) {
+            store(a, b, lds + ((t + 1) & 1) * kStage);
+            load(a, b, t + 2);
+            multiply_step(lds + (t & 1) * kStage, acc);
+            __syncthreads();
+        }
+        multiply_step(lds + (t & 1) * kStage, acc);
+    }
+
+    // The same for large tiles with two wavefronts on a SIMD, in turns: in every quarter step one of them fetches (its fragments out of LDS,
+    // a part of the next step into it) while the other multiplies, and they change places at a barrier; the second half of the block
+    // is one turn late throughout.  All that a quarter multiplies is in registers when its turn begins, so the matrix cores
+    // of a SIMD wait for LDS only where the other wavefront's fetching takes longer than the multiplying.
+    template <bool NEXT, bool PLAIN>
+    static __device__ __forceinline__ void turns_step(A &a, B &b, char *lds, int t, Acc &acc)
+    {
+        const char *from = lds + (t & 1) * kStage;
+        char *to = lds + ((t + 1) & 1) * kStage;
+        constexpr int P = (A::kPer + B::kPer) / 4;          // chunks of a quarter
+        static_assert(P * 4 == A::kPer + B::kPer, "quarters alike");
+        const char *at_a = a.step_base((t + 2) * BK), *at_b = b.step_base((t + 2) * BK);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            Vec16 fa[TM], fb[TN];
+            read(from, s, fa, fb);
+            if (NEXT) {
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = s * P; i < (s + 1) * P; ++i) {
+                    if (i < A::kPer) a.store_chunk(to, i);
+                    else b.store_chunk(to + A::kBytes, i - A::kPer);
+                }
+                if (!PLAIN && s == 3) load(a, b, t + 2);
+            }
+            // the fragments are here (LDS answers in order; what is written has to be there at the step's end only)
+            if (NEXT && PLAIN && s < 3) asm volatile("s_waitcnt lgkmcnt(%0)" :: "i"(P) : "memory");
+            else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            if (NEXT && PLAIN) {
+#pragma unroll
+                for (int i = s * P; i < (s + 1) * P; ++i) {
+                    if (i < A::kPer) a.load_chunk(at_a, i);
+                    else b.load_chunk(at_b, i - A::kPer);
+                }
+            }
+            multiply_quarter(fa, fb, acc);
+            if (NEXT && PLAIN) {
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);      // two matrix instructions,
+                    __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);      // a load
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    static __device__ __forceinline__ void run_in_turns(A &a, B &b, char *lds, Acc &acc)
+    {
+        static_assert(THREADS == 512, "wavefronts w and w + 4 share a SIMD");
+        clear(acc);
+        const int steps = (a.depth + BK - 1) / BK;
+        if (steps == 0) return;
+        a.init();
+        b.init();
+        load(a, b, 0);
+        store(a, b, lds);
+        load(a, b, 1);
+        __syncthreads();
+        const bool late = threadIdx.x >= THREADS / 2;
+        if (late) __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        int t = 0;
+        for (; t + 2 < a.depth / BK; ++t) turns_step<true, true>(a, b, lds, t, acc);
+        for (; t + 1 < steps; ++t) turns_step<true, false>(a, b, lds, t, acc);
+        turns_step<false, false>(a, b, lds, t, acc);
+        if (!late) __builtin_amdgcn_s_barrier();
+    }
+
+    // Steps [t, end) by one wavefront for itself; lds: one stage of its own.  (A wavefront's LDS accesses are in order.)
+    static __device__ __forceinline__ void run_alone(A &a, B &b, char *lds, int t, int end, Acc &acc)
+    {
+        static_assert(THREADS == 64, "one wavefront");
+        clear(acc);
+        if (t >= end) return;
+        a.init();
+        b.init();
+        load(a, b, t);
+        for (; t < end; ++t) {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            store(a, b, lds);
+            if (t + 1 < end) load(a, b, t + 1);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            multiply_step(lds, acc);
+        }
+    }
+
+    static __device__ __forceinline__ void put(const Sink &p, const Acc &acc, int64_t row0, int64_t end, int col0)
+    {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) put_tile(p, acc[i][j], row0 + wave_row() + i * 32, end, col0 + wave_col() + j * 32, lane);
     }
 };
+
+// The kinds of tiles.  LARGE: 256 x 256 in turns, bf16 and whole chunks only (its registers are full).  MEDIUM: 128 x 128, two blocks to a CU.
+// NARROW: 128 x 64, SMALL: 64 x 64, for results of few columns.
+enum Kind { LARGE, MEDIUM, NARROW, SMALL };
+constexpr int kind_rows(Kind k) { return k == LARGE ? 256 : (k == SMALL ? 64 : 128); }
+constexpr int kind_cols(Kind k) { return k == LARGE ? 256 : (k == MEDIUM ? 128 : 64); }
+constexpr int kind_threads(Kind k) { return k == LARGE ? 512 : 256; }
+template <typename T, Kind KIND, bool A_ALONG, bool B_ALONG, bool ODD>
+using KindTile = Tile<T, kind_rows(KIND), kind_cols(KIND), 2, KIND == LARGE ? 4 : 2, A_ALONG, B_ALONG, ODD>;
+
+template <typename K, Kind KIND>
+__device__ __forceinline__ void run_kind(typename K::A &a, typename K::B &b, char *lds, typename K::Acc &acc)
+{
+    if constexpr (KIND == LARGE) K::run_in_turns(a, b, lds, acc);
+    else K::run(a, b, lds, acc);
+}
 
 struct RowsArgs {
     const void *a, *w;
@@ -307,30 +530,80 @@ struct RowsArgs {
     int64_t w_group;        // elements of a group's matrix
     int32_t ld_w;
     int32_t n_groups, depth, col_tiles;
+    int32_t most;           // pieces there can be
     Sink sink;              // bias: of group 0
 };
 
-// forward and rows' gradient: pieces of BM rows of the groups x column tiles
-template <typename T, int BM, int BN, int WM, int WN, bool B_ALONG>
-__global__ __launch_bounds__(64 * WM * WN) void grouped_rows_kernel(const RowsArgs p)
+template <typename K, typename T, bool B_ALONG>
+__device__ __forceinline__ void rows_operands(const RowsArgs &p, const Span &s, int col0, typename K::A &a, typename K::B &b, Sink &sink)
 {
-    using K = Tile<T, BM, BN, WM, WN, true, B_ALONG>;
-    __shared__ __attribute__((aligned(16))) char lds[K::kLds];
-    Span s;
-    if (!find_piece(p.ptr, p.n_groups, p.n_rows, BM, static_cast<int>(blockIdx.x) / p.col_tiles, &s)) return;
-    const int col0 = static_cast<int>(blockIdx.x) % p.col_tiles * BN;
-    typename K::A a;
-    typename K::B b;
     a.base = static_cast<const T *>(p.a) + s.row * p.ld_a;
     a.ld = p.ld_a; a.rows = s.end - s.row; a.col0 = 0; a.depth = p.depth;
     const T *w = static_cast<const T *>(p.w) + s.group * p.w_group;
-    b.ld = p.ld_w; b.depth = p.depth; b.col0 = col0; b.rows = p.sink.n_cols - col0;
     b.base = B_ALONG ? w + static_cast<int64_t>(col0) * p.ld_w : w;
-    f32x16 acc[K::TM][K::TN];
-    K::run(a, b, lds, acc);
-    Sink sink = p.sink;
+    b.ld = p.ld_w; b.rows = p.sink.n_cols - col0; b.col0 = B_ALONG ? 0 : col0; b.depth = p.depth;
+    sink = p.sink;
     if (sink.bias) sink.bias += static_cast<int64_t>(s.group) * sink.n_cols;
-    K::put(sink, acc, s.row, s.end, col0);
+}
+
+// forward and rows' gradient: pieces of the groups' rows x column tiles
+template <typename T, Kind KIND, bool B_ALONG, bool ODD>
+__global__ __launch_bounds__(kind_threads(KIND)) __attribute__((amdgpu_waves_per_eu(2))) void grouped_rows_kernel(const RowsArgs p)
+{
+    using K = KindTile<T, KIND, true, B_ALONG, ODD>;
+    constexpr int BM = kind_rows(KIND), BN = kind_cols(KIND);
+    __shared__ __attribute__((aligned(16))) char lds[2 * K::kStage];
+    const int pieces = count_pieces(p.ptr, p.n_groups, p.n_rows, BM, p.most);
+    if (static_cast<int>(blockIdx.x) >= pieces * p.col_tiles) return;
+    int piece, col;
+    band_order(blockIdx.x, pieces, p.col_tiles, kBandRows / BM, &piece, &col);
+    Span s;
+    if (!find_piece(p.ptr, p.n_groups, p.n_rows, BM, piece, &s)) return;
+    typename K::A a;
+    typename K::B b;
+    Sink sink;
+    rows_operands<K, T, B_ALONG>(p, s, col * BN, a, b, sink);
+    typename K::Acc acc;
+    run_kind<K, KIND>(a, b, lds, acc);
+    K::put(sink, acc, s.row, s.end, col * BN);
+}
+
+// The same where a group has few rows, and what takes the time is reading its weights: tiles of 32 x 64 by WAVES wavefronts, which share
+// the depth, each for itself and without a barrier until their sums meet in LDS, in order.
+template <typename T, int WAVES, bool B_ALONG, bool ODD>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void grouped_few_rows_kernel(const RowsArgs p)
+{
+    using K = Tile<T, 32, 64, 1, 1, true, B_ALONG, ODD>;
+    constexpr int kSums = 2 * 16 * 64 * 4;
+    static_assert(K::kStage >= kSums, "a wavefront's sums fit where its tiles were");
+    __shared__ __attribute__((aligned(16))) char lds[WAVES * K::kStage];
+    Span s;
+    if (!find_piece(p.ptr, p.n_groups, p.n_rows, 32, static_cast<int>(blockIdx.x) / p.col_tiles, &s)) return;
+    const int col0 = static_cast<int>(blockIdx.x) % p.col_tiles * 64, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    typename K::A a;
+    typename K::B b;
+    Sink sink;
+    rows_operands<K, T, B_ALONG>(p, s, col0, a, b, sink);
+    typename K::Acc acc;
+    const int steps = (p.depth + K::BK - 1) / K::BK;
+    K::run_alone(a, b, lds + wave * K::kStage, wave * steps / WAVES, (wave + 1) * steps / WAVES, acc);
+    __syncthreads();
+    float *sums = reinterpret_cast<float *>(lds);
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sums[((wave * 2 + j) * 16 + r) * 64 + lane] = acc[0][j][r];
+    __syncthreads();
+    if (wave >= 2) return;
+    // wavefront j takes the sums of 32 columns
+    f32x16 all;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        all[r] = sums[(wave * 16 + r) * 64 + lane];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) all[r] += sums[((w * 2 + wave) * 16 + r) * 64 + lane];
+    }
+    put_tile(sink, all, s.row, s.end, col0 + wave * 32, lane);
 }
 
 struct WeightArgs {
@@ -343,110 +616,200 @@ struct WeightArgs {
 };
 
 // weights' gradient: tiles of [d_in x d_out] per group, or per piece of `step` rows (partial sums, joined by sum_pieces_kernel)
-template <typename T, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void grouped_weight_kernel(const WeightArgs p)
+template <typename T, Kind KIND, bool ODD>
+__global__ __launch_bounds__(kind_threads(KIND)) __attribute__((amdgpu_waves_per_eu(2))) void grouped_weight_kernel(const WeightArgs p)
 {
-    using K = Tile<T, BM, BN, WM, WN, false, false>;
-    __shared__ __attribute__((aligned(16))) char lds[K::kLds];
-    const int64_t tiles = static_cast<int64_t>(p.row_tiles) * p.col_tiles;
-    const int64_t index = blockIdx.x / tiles, tile = blockIdx.x % tiles;
+    using K = KindTile<T, KIND, false, false, ODD>;
+    constexpr int BM = kind_rows(KIND), BN = kind_cols(KIND);
+    __shared__ __attribute__((aligned(16))) char lds[2 * K::kStage];
+    const int tiles = p.row_tiles * p.col_tiles, index = static_cast<int>(blockIdx.x) / tiles;
     Span s;
     if (p.step) {
-        if (!find_piece(p.ptr, p.n_groups, p.n_rows, p.step, static_cast<int>(index), &s)) return;
+        if (!find_piece(p.ptr, p.n_groups, p.n_rows, p.step, index, &s)) return;
     } else {
-        s.group = static_cast<int>(index);
+        s.group = index;
         group_range(p.ptr, s.group, p.n_groups, p.n_rows, &s.row, &s.end);
     }
-    const int row0 = static_cast<int>(tile / p.col_tiles) * BM, col0 = static_cast<int>(tile % p.col_tiles) * BN;
+    int row, col;
+    band_order(static_cast<int>(blockIdx.x) % tiles, p.row_tiles, p.col_tiles, kBandRows / BM, &row, &col);
+    const int row0 = row * BM, col0 = col * BN;
     typename K::A a;
     typename K::B b;
     a.base = static_cast<const T *>(p.a) + s.row * p.ld_a;
     a.ld = p.ld_a; a.rows = p.d_in - row0; a.col0 = row0; a.depth = s.end - s.row;
     b.base = static_cast<const T *>(p.dz) + s.row * p.ld_dz;
     b.ld = p.ld_dz; b.rows = p.d_out - col0; b.col0 = col0; b.depth = a.depth;
-    f32x16 acc[K::TM][K::TN];
-    K::run(a, b, lds, acc);
+    typename K::Acc acc;
+    run_kind<K, KIND>(a, b, lds, acc);
     Sink sink = p.sink;
-    const int64_t first = index * p.d_in;
+    const int64_t first = static_cast<int64_t>(index) * p.d_in;
     sink.out = static_cast<char *>(sink.out) + first * p.d_out * (sink.bf16 ? 2 : 4);
     K::put(sink, acc, row0, p.d_in, col0);
 }
 
-// out[g] (+)= the sum of the partial sums of the group's pieces, front to back; `width` values each
+// ---- widths of less than 16 bytes: plain sums ------------------------------------------------------------------
+__device__ __forceinline__ void put1(const Sink &p, float v, int64_t row, int col)
+{
+    if (p.bias) v += p.bias[col];
+    if (p.relu && v < 0.f) v = 0.f;
+    if (p.bf16) {
+        Bf16 *o = static_cast<Bf16 *>(p.out) + row * p.ld + col;
+        from_f32(v + (p.add ? to_f32(*o) : 0.f), *o);
+    } else {
+        float *o = static_cast<float *>(p.out) + row * p.ld + col;
+        *o = v + (p.add ? *o : 0.f);
+    }
+}
+
+// blocks of 64 rows of a group; a thread per element
+template <typename T, bool B_ALONG>
+__global__ __launch_bounds__(256) void tiny_rows_kernel(const RowsArgs p)
+{
+    Span s;
+    if (!find_piece(p.ptr, p.n_groups, p.n_rows, 64, static_cast<int>(blockIdx.x) / p.col_tiles, &s)) return;
+    const T *w = static_cast<const T *>(p.w) + s.group * p.w_group;
+    Sink sink = p.sink;
+    if (sink.bias) sink.bias += static_cast<int64_t>(s.group) * sink.n_cols;
+    const int col0 = static_cast<int>(blockIdx.x) % p.col_tiles * 64, cols = min(64, sink.n_cols - col0);
+    for (int e = threadIdx.x; e < (s.end - s.row) * cols; e += 256) {
+        const int64_t row = s.row + e / cols;
+        const int col = col0 + e % cols;
+        const T *a = static_cast<const T *>(p.a) + row * p.ld_a;
+        float sum = 0.f;
+        for (int k = 0; k < p.depth; ++k) sum += to_f32(a[k]) * to_f32(B_ALONG ? w[static_cast<int64_t>(col) * p.ld_w + k] : w[static_cast<int64_t>(k) * p.ld_w + col]);
+        put1(sink, sum, row, col);
+    }
+}
+
+// a block per group or piece and 256 elements of the result
+template <typename T>
+__global__ __launch_bounds__(256) void tiny_weight_kernel(const WeightArgs p)
+{
+    const int tiles = p.row_tiles * p.col_tiles, index = static_cast<int>(blockIdx.x) / tiles;
+    Span s;
+    if (p.step) {
+        if (!find_piece(p.ptr, p.n_groups, p.n_rows, p.step, index, &s)) return;
+    } else {
+        s.group = index;
+        group_range(p.ptr, s.group, p.n_groups, p.n_rows, &s.row, &s.end);
+    }
+    const int64_t e = static_cast<int64_t>(blockIdx.x % tiles) * 256 + threadIdx.x;
+    if (e >= static_cast<int64_t>(p.d_in) * p.d_out) return;
+    const int k = static_cast<int>(e / p.d_out), n = static_cast<int>(e % p.d_out);
+    float sum = 0.f;
+    for (int64_t r = s.row; r < s.end; ++r) sum += to_f32(static_cast<const T *>(p.a)[r * p.ld_a + k]) * to_f32(static_cast<const T *>(p.dz)[r * p.ld_dz + n]);
+    Sink sink = p.sink;
+    sink.out = static_cast<char *>(sink.out) + static_cast<int64_t>(index) * p.d_in * p.d_out * (sink.bf16 ? 2 : 4);
+    put1(sink, sum, k, n);
+}
+
+// out[g] (+)= the sum of the partial sums of the group's pieces, `width` values each: a wavefront adds up a quarter of them, front to back
 struct JoinArgs {
     const float *part;
     const int64_t *ptr;
     void *out;
     int64_t n_rows, width;
-    int32_t n_groups, step, bf16, add;
+    int32_t n_groups, step, most, bf16, add;
 };
 __global__ __launch_bounds__(256) void sum_pieces_kernel(const JoinArgs p)
 {
-    const int g = blockIdx.y;
-    const int lane = threadIdx.x & 63;
-    int first = 0;
-    for (int g0 = 0; g0 < g; g0 += kWave) {
-        int32_t lo, hi;
-        group_range(p.ptr, g0 + lane, g0 + lane < g ? p.n_groups : 0, p.n_rows, &lo, &hi);
-        first += (hi - lo) / p.step + ((hi - lo) % p.step != 0);
-    }
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) first += __shfl_xor(first, off);
+    __shared__ float joined[4][64];
+    const int g = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int32_t lo, hi;
     group_range(p.ptr, g, p.n_groups, p.n_rows, &lo, &hi);
-    const int count = (hi - lo) / p.step + ((hi - lo) % p.step != 0);
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (c >= p.width) return;
+    // (overlapping groups could have more pieces than there is room for)
+    const int first = count_pieces(p.ptr, g, p.n_rows, p.step, p.most), count = min(pieces_in(hi - lo, p.step), p.most - first);
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * 64 + lane;
     float sum = 0.f;
-#pragma unroll 4
-    for (int i = 0; i < count; ++i) sum += p.part[(first + i) * p.width + c];
+    if (c < p.width) {
+        const int to = (wave + 1) * count / 4;
+#pragma unroll 8
+        for (int i = wave * count / 4; i < to; ++i) sum += p.part[(first + i) * p.width + c];
+    }
+    joined[wave][lane] = sum;
+    __syncthreads();
+    if (wave != 0 || c >= p.width) return;
+    sum = joined[0][lane] + joined[1][lane] + joined[2][lane] + joined[3][lane];
     const int64_t at = static_cast<int64_t>(g) * p.width + c;
     if (p.bf16) { Bf16 *o = static_cast<Bf16 *>(p.out) + at; from_f32(sum + (p.add ? to_f32(*o) : 0.f), *o); }
     else { float *o = static_cast<float *>(p.out) + at; *o = sum + (p.add ? *o : 0.f); }
 }
 
-// dz = grad_out where out > 0 (RELU; written for the two products), and its column sums over pieces of rows
+// dz = grad_out where out > 0 (RELU; written for the two products), and its column sums over pieces of rows.  Bound by HBM.
+constexpr int kMaskRows = 128;
 struct MaskArgs {
     const void *grad, *out;
     void *dz;               // NULL: grad is dz already
     float *part;            // NULL: no column sums
     const int64_t *ptr;
     int64_t n_rows, ld_grad, ld_out, ld_dz;
-    int32_t n_groups, d_out, step, out_bf16;
+    int32_t n_groups, d_out, out_bf16, lanes_log2;
 };
-template <typename T>
+// 2^lanes_log2 lanes take a row, V columns each; a wavefront 64 / 2^lanes_log2 rows at a time
+template <typename T, int V>
 __global__ __launch_bounds__(256) void mask_rows_kernel(const MaskArgs p)
 {
-    __shared__ float joined[4][64];
+    __shared__ float joined[256 * V];
     Span s;
-    if (!find_piece(p.ptr, p.n_groups, p.n_rows, p.step, static_cast<int>(blockIdx.x), &s)) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int64_t c0 = static_cast<int64_t>(blockIdx.y) * 64; c0 < p.d_out; c0 += static_cast<int64_t>(gridDim.y) * 64) {
-        const int64_t c = c0 + lane;
-        float sum = 0.f;
-        if (c < p.d_out)
-            for (int64_t r = s.row + wave; r < s.end; r += 4) {
-                T g = static_cast<const T *>(p.grad)[r * p.ld_grad + c];
+    if (!find_piece(p.ptr, p.n_groups, p.n_rows, kMaskRows, static_cast<int>(blockIdx.x), &s)) return;
+    const int lanes = 1 << p.lanes_log2, groups = 256 >> p.lanes_log2, group = threadIdx.x >> p.lanes_log2;
+    const int64_t c = ((static_cast<int64_t>(blockIdx.y) << p.lanes_log2) + (threadIdx.x & (lanes - 1))) * V;
+    const int64_t col = c + V <= p.d_out ? c : p.d_out - V;         // the last vector ends with the row; the columns before c are its neighbour's
+    float sum[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) sum[e] = 0.f;
+    if (c < p.d_out) {
+        constexpr int U = 4;
+        for (int64_t r0 = s.row + group; r0 < s.end; r0 += U * groups) {
+            float g[U][V], o[U][V];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t r = min(r0 + u * groups, static_cast<int64_t>(s.end) - 1);
+                load_n<V>(static_cast<const T *>(p.grad) + r * p.ld_grad + col, g[u]);
                 if (p.out) {
-                    const float o = p.out_bf16 ? to_f32(static_cast<const Bf16 *>(p.out)[r * p.ld_out + c]) : static_cast<const float *>(p.out)[r * p.ld_out + c];
-                    if (!(o > 0.f)) from_f32(0.f, g);
+                    if (p.out_bf16) load_n<V>(static_cast<const Bf16 *>(p.out) + r * p.ld_out + col, o[u]);
+                    else load_n<V>(static_cast<const float *>(p.out) + r * p.ld_out + col, o[u]);
                 }
-                if (p.dz) static_cast<T *>(p.dz)[r * p.ld_dz + c] = g;
-                sum += to_f32(g);
             }
-        if (p.part) {
-            joined[wave][lane] = sum;
-            __syncthreads();
-            if (wave == 0 && c < p.d_out) p.part[static_cast<int64_t>(blockIdx.x) * p.d_out + c] = joined[0][lane] + joined[1][lane] + joined[2][lane] + joined[3][lane];
-            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (r0 + u * groups >= s.end) break;
+                if (p.out) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) g[u][e] = o[u][e] > 0.f ? g[u][e] : 0.f;
+                }
+                if (p.dz) store_n<V>(static_cast<T *>(p.dz) + (r0 + u * groups) * p.ld_dz + col, g[u]);
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum[e] += g[u][e];
+            }
         }
     }
+    if (!p.part) return;
+#pragma unroll
+    for (int e = 0; e < V; ++e) joined[e * 256 + threadIdx.x] = sum[e];
+    __syncthreads();
+    if (group != 0 || c >= p.d_out) return;
+    for (int i = 1; i < groups; ++i) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum[e] += joined[e * 256 + (i << p.lanes_log2) + threadIdx.x];
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+        if (col + e >= c) p.part[static_cast<int64_t>(blockIdx.x) * p.d_out + col + e] = sum[e];
 }
 
-constexpr int kMaskRows = 256;
+// ---- which tiles ---------------------------------------------------------------------------------------------
+constexpr int kCus = 256;
+
+// LARGE or MEDIUM, by how often the chip is filled: a CU takes one large tile at a time or two medium ones, and a large one (four
+// times the work) takes some 2.9 times as long as a medium one beside another
+bool large_pays(int64_t large_tiles, int64_t medium_tiles) { return ceil_div(large_tiles, kCus) * 29 <= ceil_div(medium_tiles, 2 * kCus) * 20; }
 
 struct GradPlan {
+    bool tiny;
+    Kind kind;
     int32_t step;                   // rows of a piece of the weights' gradient, 0: groups whole
+    int64_t row_tiles, col_tiles;
     int64_t pieces, mask_pieces;    // at most
     int64_t ld_dz;
     size_t dz, part, bias_part, bytes;
@@ -454,18 +817,25 @@ struct GradPlan {
 
 GradPlan plan_grad(int64_t n_rows, int32_t n_groups, int32_t d_in, int32_t d_out, mgg_dtype_t dtype, bool relu)
 {
-    GradPlan g;
-    const int64_t tiles = ceil_div(d_in, 128) * ceil_div(d_out, 128);
-    g.step = 0;
+    GradPlan g{};
+    const int32_t chunk = dtype == MGG_BF16 ? 8 : 4;
+    const int64_t present = n_groups < n_rows ? n_groups : n_rows;      // groups that can have rows
+    g.tiny = d_in < chunk || d_out < chunk;
+    g.kind = d_out > 64 ? MEDIUM : (d_in > 64 ? NARROW : SMALL);
+    if (dtype == MGG_BF16 && g.kind == MEDIUM && d_in % chunk == 0 && d_out % chunk == 0 &&
+        large_pays(n_groups * ceil_div(d_in, 256) * ceil_div(d_out, 256), n_groups * ceil_div(d_in, 128) * ceil_div(d_out, 128)))
+        g.kind = LARGE;
+    g.row_tiles = g.tiny ? ceil_div(static_cast<int64_t>(d_in) * d_out, 256) : ceil_div(d_in, kind_rows(g.kind));
+    g.col_tiles = g.tiny ? 1 : ceil_div(d_out, kind_cols(g.kind));
+    // pieces of rows where the tiles of the groups do not fill the chip (counted as if one group had all rows)
+    const int64_t tiles = g.row_tiles * g.col_tiles;
     g.pieces = n_groups;
-    if (tiles < 256 && n_rows > 0) {
-        const int64_t wanted = ceil_div(512, tiles);
-        int64_t step = ceil_div(ceil_div(n_rows, wanted), 64) * 64;
-        if (step < 256) step = 256;
-        g.step = static_cast<int32_t>(step < (1 << 30) ? step : 1 << 30);
-        g.pieces = n_rows / g.step + (n_groups < n_rows ? n_groups : n_rows);
+    if (g.kind != LARGE && tiles < kCus && n_rows > 0) {
+        const int64_t step = ceil_div(ceil_div(n_rows, ceil_div(2 * kCus, tiles)), 64) * 64;
+        g.step = static_cast<int32_t>(step < 256 ? 256 : (step < (1 << 30) ? step : 1 << 30));
+        g.pieces = n_rows / g.step + present;
     }
-    g.mask_pieces = n_rows / kMaskRows + (n_groups < n_rows ? n_groups : n_rows);
+    g.mask_pieces = n_rows / kMaskRows + present;
     g.ld_dz = static_cast<int64_t>(round_up(static_cast<size_t>(d_out), 8));
     size_t at = 0;
     g.dz = at; at += relu ? round_up(static_cast<size_t>(n_rows) * g.ld_dz * (dtype == MGG_BF16 ? 2 : 4), 256) : 0;
@@ -475,40 +845,108 @@ GradPlan plan_grad(int64_t n_rows, int32_t n_groups, int32_t d_in, int32_t d_out
     return g;
 }
 
-template <typename T>
-mgg_status_t rows_product(RowsArgs p, bool b_along, hipStream_t stream)
+mgg_status_t launched(const char *what)
 {
-    constexpr int BM = 128, BN = 128;
-    p.col_tiles = static_cast<int32_t>(ceil_div(p.sink.n_cols, BN));
-    const int64_t blocks = (p.n_rows / BM + (p.n_groups < p.n_rows ? p.n_groups : p.n_rows)) * p.col_tiles;
-    if (blocks > INT32_MAX) return fail(MGG_ERR_UNSUPPORTED, "too many tiles for one launch");
-    const dim3 grid(static_cast<unsigned>(blocks));
-    if (b_along) hipLaunchKernelGGL((grouped_rows_kernel<T, BM, BN, 2, 2, true>), grid, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((grouped_rows_kernel<T, BM, BN, 2, 2, false>), grid, dim3(256), 0, stream, p);
     const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? MGG_OK : hip_fail(e, "grouped product launch");
+    return e == hipSuccess ? MGG_OK : hip_fail(e, what);
+}
+
+template <typename T, bool B_ALONG, bool ODD>
+mgg_status_t rows_product(RowsArgs p, hipStream_t stream)
+{
+    constexpr int N = Elem<T>::N;
+    const int32_t cols = p.sink.n_cols;
+    const int64_t present = p.n_groups < p.n_rows ? p.n_groups : p.n_rows;
+    auto grid = [&](int rows, int tile_cols) {
+        p.col_tiles = static_cast<int32_t>(ceil_div(cols, tile_cols));
+        const int64_t most = p.n_rows / rows + present;
+        p.most = static_cast<int32_t>(most < INT32_MAX ? most : INT32_MAX);
+        return most * p.col_tiles;
+    };
+    const char *const refused = "too many tiles for one launch";
+#define MGG_GRID(ROWS, COLS)                                                         \
+    const int64_t blocks = grid(ROWS, COLS);                                         \
+    if (blocks > INT32_MAX) return fail(MGG_ERR_UNSUPPORTED, "%s", refused);          \
+    const dim3 blocks_dim(static_cast<unsigned>(blocks))
+    if (cols < N || p.depth < N) {
+        MGG_GRID(64, 64);
+        hipLaunchKernelGGL((tiny_rows_kernel<T, B_ALONG>), blocks_dim, dim3(256), 0, stream, p);
+        return launched("grouped product launch");
+    }
+    // few rows to a group: reading the weights is what takes the time
+    if (p.n_rows <= 24 * static_cast<int64_t>(p.n_groups) || p.n_rows <= 64) {
+        MGG_GRID(32, 64);
+        if (blocks < 2 * kCus) hipLaunchKernelGGL((grouped_few_rows_kernel<T, 8, B_ALONG, ODD>), blocks_dim, dim3(512), 0, stream, p);
+        else hipLaunchKernelGGL((grouped_few_rows_kernel<T, 4, B_ALONG, ODD>), blocks_dim, dim3(256), 0, stream, p);
+        return launched("grouped product launch");
+    }
+    if constexpr (!ODD && sizeof(T) == 2) {
+        // (a group's last piece is half full on average)
+        if (large_pays((p.n_rows / 256 + present / 2) * ceil_div(cols, 256), (p.n_rows / 128 + present / 2) * ceil_div(cols, 128))) {
+            MGG_GRID(256, 256);
+            hipLaunchKernelGGL((grouped_rows_kernel<T, LARGE, B_ALONG, ODD>), blocks_dim, dim3(512), 0, stream, p);
+            return launched("grouped product launch");
+        }
+    }
+    if (cols <= 64) {
+        MGG_GRID(128, 64);
+        hipLaunchKernelGGL((grouped_rows_kernel<T, NARROW, B_ALONG, ODD>), blocks_dim, dim3(256), 0, stream, p);
+    } else {
+        MGG_GRID(128, 128);
+        hipLaunchKernelGGL((grouped_rows_kernel<T, MEDIUM, B_ALONG, ODD>), blocks_dim, dim3(256), 0, stream, p);
+    }
+#undef MGG_GRID
+    return launched("grouped product launch");
 }
 
 template <typename T>
-mgg_status_t weight_product(WeightArgs p, int64_t pieces, hipStream_t stream)
+mgg_status_t rows_product_of(const RowsArgs &p, bool b_along, hipStream_t stream)
 {
-    constexpr int BM = 128, BN = 128;
-    p.row_tiles = static_cast<int32_t>(ceil_div(p.d_in, BM));
-    p.col_tiles = static_cast<int32_t>(ceil_div(p.d_out, BN));
-    const int64_t blocks = pieces * p.row_tiles * p.col_tiles;
-    if (blocks > INT32_MAX) return fail(MGG_ERR_UNSUPPORTED, "too many tiles for one launch");
-    hipLaunchKernelGGL((grouped_weight_kernel<T, BM, BN, 2, 2>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, p);
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? MGG_OK : hip_fail(e, "grouped weight gradient launch");
+    const bool odd = p.depth % Elem<T>::N != 0 || p.sink.n_cols % Elem<T>::N != 0;
+    if (b_along) return odd ? rows_product<T, true, true>(p, stream) : rows_product<T, true, false>(p, stream);
+    return odd ? rows_product<T, false, true>(p, stream) : rows_product<T, false, false>(p, stream);
+}
+
+template <typename T, bool ODD>
+mgg_status_t weight_product(WeightArgs p, const GradPlan &g, hipStream_t stream)
+{
+    p.row_tiles = static_cast<int32_t>(g.row_tiles);
+    p.col_tiles = static_cast<int32_t>(g.col_tiles);
+    if (g.row_tiles > INT32_MAX || g.pieces * g.row_tiles > INT32_MAX / g.col_tiles) return fail(MGG_ERR_UNSUPPORTED, "too many tiles for one launch");
+    const dim3 grid(static_cast<unsigned>(g.pieces * g.row_tiles * g.col_tiles));
+    if (g.tiny) hipLaunchKernelGGL((tiny_weight_kernel<T>), grid, dim3(256), 0, stream, p);
+    else if (g.kind == MEDIUM) hipLaunchKernelGGL((grouped_weight_kernel<T, MEDIUM, ODD>), grid, dim3(256), 0, stream, p);
+    else if (g.kind == NARROW) hipLaunchKernelGGL((grouped_weight_kernel<T, NARROW, ODD>), grid, dim3(256), 0, stream, p);
+    else if (g.kind == SMALL) hipLaunchKernelGGL((grouped_weight_kernel<T, SMALL, ODD>), grid, dim3(256), 0, stream, p);
+    else if constexpr (!ODD && sizeof(T) == 2) hipLaunchKernelGGL((grouped_weight_kernel<T, LARGE, ODD>), grid, dim3(512), 0, stream, p);
+    return launched("grouped weight gradient launch");
+}
+
+template <typename T>
+mgg_status_t weight_product_of(const WeightArgs &p, const GradPlan &g, hipStream_t stream)
+{
+    return p.d_in % Elem<T>::N != 0 || p.d_out % Elem<T>::N != 0 ? weight_product<T, true>(p, g, stream) : weight_product<T, false>(p, g, stream);
 }
 
 mgg_status_t join_pieces(const JoinArgs &p, hipStream_t stream)
 {
-    const int64_t blocks = ceil_div(p.width, 256);
+    const int64_t blocks = ceil_div(p.width, 64);
     if (blocks > INT32_MAX) return fail(MGG_ERR_UNSUPPORTED, "too many columns for one launch");
     hipLaunchKernelGGL(sum_pieces_kernel, dim3(static_cast<unsigned>(blocks), p.n_groups), dim3(256), 0, stream, p);
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? MGG_OK : hip_fail(e, "partial sum launch");
+    return launched("partial sum launch");
+}
+
+template <typename T>
+mgg_status_t mask_rows(MaskArgs m, int64_t pieces, hipStream_t stream)
+{
+    constexpr int V = 16 / sizeof(T);
+    const int64_t vecs = m.d_out < V ? m.d_out : ceil_div(m.d_out, V);
+    m.lanes_log2 = ceil_log2(vecs) < 6 ? ceil_log2(vecs) : 6;
+    const dim3 grid(static_cast<unsigned>(pieces), static_cast<unsigned>(ceil_div(vecs, static_cast<int64_t>(1) << m.lanes_log2)));
+    if (grid.y > 65535) return fail(MGG_ERR_UNSUPPORTED, "too many columns for one launch");
+    if (m.d_out < V) hipLaunchKernelGGL((mask_rows_kernel<T, 1>), grid, dim3(256), 0, stream, m);
+    else hipLaunchKernelGGL((mask_rows_kernel<T, V>), grid, dim3(256), 0, stream, m);
+    return launched("mask launch");
 }
 
 }  // namespace
@@ -521,7 +959,7 @@ mgg_status_t launch_update_grouped(int64_t n_rows, int32_t n_groups, const int64
     p.a = a; p.w = w; p.ptr = group_ptr; p.n_rows = n_rows; p.ld_a = ld_a; p.n_groups = n_groups;
     p.w_group = static_cast<int64_t>(d_in) * d_out; p.ld_w = d_out; p.depth = d_in;
     p.sink = Sink{out, ld_out, bias, d_out, out_dtype == MGG_BF16, relu, 0};
-    return dtype == MGG_BF16 ? rows_product<Bf16>(p, false, stream) : rows_product<float>(p, false, stream);
+    return dtype == MGG_BF16 ? rows_product_of<Bf16>(p, false, stream) : rows_product_of<float>(p, false, stream);
 }
 
 size_t grouped_grad_workspace(int64_t n_rows, int32_t n_groups, int32_t d_in, int32_t d_out, mgg_dtype_t dtype, bool relu)
@@ -537,23 +975,20 @@ mgg_status_t launch_update_grouped_grad(const GroupedGrad &q, void *workspace, h
     const void *dz = q.grad_out;
     int64_t ld_dz = q.ld_grad;
     mgg_status_t s = MGG_OK;
-    if (q.n_rows > 0 && (q.relu || q.grad_bias) && (q.grad_a || q.grad_w || q.grad_bias)) {
+    if (q.n_rows > 0 && (q.grad_bias || (q.relu && (q.grad_a || q.grad_w)))) {
         MaskArgs m{};
-        m.grad = q.grad_out; m.ptr = q.group_ptr; m.n_rows = q.n_rows; m.ld_grad = q.ld_grad; m.n_groups = q.n_groups; m.d_out = q.d_out; m.step = kMaskRows;
+        m.grad = q.grad_out; m.ptr = q.group_ptr; m.n_rows = q.n_rows; m.ld_grad = q.ld_grad; m.n_groups = q.n_groups; m.d_out = q.d_out;
         if (q.relu) {
             m.out = q.out; m.ld_out = q.ld_out; m.out_bf16 = q.out_dtype == MGG_BF16;
             if (q.grad_a || q.grad_w) { m.dz = ws + g.dz; m.ld_dz = g.ld_dz; dz = m.dz; ld_dz = m.ld_dz; }
         }
         if (q.grad_bias) m.part = reinterpret_cast<float *>(ws + g.bias_part);
-        const int64_t slabs = ceil_div(q.d_out, 64);
-        const dim3 grid(static_cast<unsigned>(g.mask_pieces), static_cast<unsigned>(slabs < 1024 ? slabs : 1024));
-        if (bf16) hipLaunchKernelGGL(mask_rows_kernel<Bf16>, grid, dim3(256), 0, stream, m);
-        else hipLaunchKernelGGL(mask_rows_kernel<float>, grid, dim3(256), 0, stream, m);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return hip_fail(e, "mask launch");
+        s = bf16 ? mask_rows<Bf16>(m, g.mask_pieces, stream) : mask_rows<float>(m, g.mask_pieces, stream);
+        if (s != MGG_OK) return s;
     }
     if (q.grad_bias) {
-        s = join_pieces(JoinArgs{reinterpret_cast<float *>(ws + g.bias_part), q.group_ptr, q.grad_bias, q.n_rows, q.d_out, q.n_groups, kMaskRows, 0, q.add_bias}, stream);
+        s = join_pieces(JoinArgs{reinterpret_cast<float *>(ws + g.bias_part), q.group_ptr, q.grad_bias, q.n_rows, q.d_out, q.n_groups, kMaskRows,
+                                 static_cast<int32_t>(g.mask_pieces), 0, q.add_bias}, stream);
         if (s != MGG_OK) return s;
     }
     if (q.grad_a) {
@@ -561,7 +996,7 @@ mgg_status_t launch_update_grouped_grad(const GroupedGrad &q, void *workspace, h
         p.a = dz; p.w = q.w; p.ptr = q.group_ptr; p.n_rows = q.n_rows; p.ld_a = ld_dz; p.n_groups = q.n_groups;
         p.w_group = static_cast<int64_t>(q.d_in) * q.d_out; p.ld_w = q.d_out; p.depth = q.d_out;
         p.sink = Sink{q.grad_a, q.ld_grad_a, nullptr, q.d_in, q.grad_a_dtype == MGG_BF16, 0, 0};
-        s = bf16 ? rows_product<Bf16>(p, true, stream) : rows_product<float>(p, true, stream);
+        s = bf16 ? rows_product_of<Bf16>(p, true, stream) : rows_product_of<float>(p, true, stream);
         if (s != MGG_OK) return s;
     }
     if (q.grad_w) {
@@ -570,10 +1005,10 @@ mgg_status_t launch_update_grouped_grad(const GroupedGrad &q, void *workspace, h
         p.n_groups = q.n_groups; p.d_in = q.d_in; p.d_out = q.d_out; p.step = g.step;
         if (g.step) p.sink = Sink{ws + g.part, q.d_out, nullptr, q.d_out, 0, 0, 0};
         else p.sink = Sink{q.grad_w, q.d_out, nullptr, q.d_out, q.grad_w_dtype == MGG_BF16, 0, q.add_w};
-        s = bf16 ? weight_product<Bf16>(p, g.pieces, stream) : weight_product<float>(p, g.pieces, stream);
+        s = bf16 ? weight_product_of<Bf16>(p, g, stream) : weight_product_of<float>(p, g, stream);
         if (s != MGG_OK || !g.step) return s;
         s = join_pieces(JoinArgs{reinterpret_cast<float *>(ws + g.part), q.group_ptr, q.grad_w, q.n_rows, static_cast<int64_t>(q.d_in) * q.d_out, q.n_groups, g.step,
-                                 q.grad_w_dtype == MGG_BF16, q.add_w}, stream);
+                                 static_cast<int32_t>(g.pieces), q.grad_w_dtype == MGG_BF16, q.add_w}, stream);
     }
     return s;
 }
