@@ -302,8 +302,15 @@ __device__ __forceinline__ void put_tile(const Sink &p, const f32x16 &acc, int64
         const int col = col0 + 16 * q + 8 * (lane >> 5);
         if (r >= end || col >= p.n_cols) continue;
         if (p.bias) {
+            float b[8];
+            if (col + 8 <= p.n_cols) {
+                load_n<8>(p.bias + col, b);
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += p.bias[col + e < p.n_cols ? col + e : p.n_cols - 1];
+                for (int e = 0; e < 8; ++e) b[e] = p.bias[min(col + e, p.n_cols - 1)];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += b[e];
         }
         if (p.relu) {
 #pragma unroll
@@ -488,6 +495,14 @@ struct Tile {
         a.init();
         b.init();
         load(a, b, t);
+        const int plain = min(end, a.depth / BK);
+        for (; t + 1 < plain; ++t) {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            store(a, b, lds);
+            load_plain(a, b, t + 1);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            multiply_step(lds, acc);
+        }
         for (; t < end; ++t) {
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             store(a, b, lds);
@@ -508,7 +523,8 @@ struct Tile {
 };
 
 // The kinds of tiles.  LARGE: 256 x 256 in turns, bf16 and whole chunks only (its registers are full).  MEDIUM: 128 x 128, two blocks to a CU.
-// NARROW: 128 x 64, SMALL: 64 x 64, for results of few columns.
+// NARROW: 128 x 64, SMALL: 64 x 64, for results of few columns; SMALL for all of fp32, too, whose products take so long that what counts is how
+// evenly the chip is filled (20 k rows 512 -> 512 over 10 groups: 106 us against 132 with MEDIUM).
 enum Kind { LARGE, MEDIUM, NARROW, SMALL };
 constexpr int kind_rows(Kind k) { return k == LARGE ? 256 : (k == SMALL ? 64 : 128); }
 constexpr int kind_cols(Kind k) { return k == LARGE ? 256 : (k == MEDIUM ? 128 : 64); }
@@ -568,18 +584,19 @@ __global__ __launch_bounds__(kind_threads(KIND)) __attribute__((amdgpu_waves_per
     K::put(sink, acc, s.row, s.end, col * BN);
 }
 
-// The same where a group has few rows, and what takes the time is reading its weights: tiles of 32 x 64 by WAVES wavefronts, which share
+// The same where a group has few rows, and what takes the time is reading its weights: tiles of 32 x BN by WAVES wavefronts, which share
 // the depth, each for itself and without a barrier until their sums meet in LDS, in order.
-template <typename T, int WAVES, bool B_ALONG, bool ODD>
+template <typename T, int BN, int WAVES, bool B_ALONG, bool ODD>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void grouped_few_rows_kernel(const RowsArgs p)
 {
-    using K = Tile<T, 32, 64, 1, 1, true, B_ALONG, ODD>;
-    constexpr int kSums = 2 * 16 * 64 * 4;
+    using K = Tile<T, 32, BN, 1, 1, true, B_ALONG, ODD>;
+    constexpr int J = BN / 32, kSums = J * 16 * 64 * 4;
+    static_assert(WAVES >= J, "a wavefront per 32 columns at the end");
     static_assert(K::kStage >= kSums, "a wavefront's sums fit where its tiles were");
     __shared__ __attribute__((aligned(16))) char lds[WAVES * K::kStage];
     Span s;
     if (!find_piece(p.ptr, p.n_groups, p.n_rows, 32, static_cast<int>(blockIdx.x) / p.col_tiles, &s)) return;
-    const int col0 = static_cast<int>(blockIdx.x) % p.col_tiles * 64, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int col0 = static_cast<int>(blockIdx.x) % p.col_tiles * BN, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     typename K::A a;
     typename K::B b;
     Sink sink;
@@ -590,18 +607,18 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
     __syncthreads();
     float *sums = reinterpret_cast<float *>(lds);
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < J; ++j)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sums[((wave * 2 + j) * 16 + r) * 64 + lane] = acc[0][j][r];
+        for (int r = 0; r < 16; ++r) sums[((wave * J + j) * 16 + r) * 64 + lane] = acc[0][j][r];
     __syncthreads();
-    if (wave >= 2) return;
+    if (wave >= J) return;
     // wavefront j takes the sums of 32 columns
     f32x16 all;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
         all[r] = sums[(wave * 16 + r) * 64 + lane];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) all[r] += sums[((w * 2 + wave) * 16 + r) * 64 + lane];
+        for (int w = 1; w < WAVES; ++w) all[r] += sums[((w * J + wave) * 16 + r) * 64 + lane];
     }
     put_tile(sink, all, s.row, s.end, col0 + wave * 32, lane);
 }
@@ -612,10 +629,34 @@ struct WeightArgs {
     int64_t n_rows, ld_a, ld_dz;
     int32_t n_groups, d_in, d_out, row_tiles, col_tiles;
     int32_t step;           // rows of a piece; 0: a group is one
-    Sink sink;              // of group or piece 0
+    Sink sink;              // of group 0
+    float *part;            // of piece 0
 };
 
-// weights' gradient: tiles of [d_in x d_out] per group, or per piece of `step` rows (partial sums, joined by sum_pieces_kernel)
+// The rows of group or piece number `index`, and where its product goes: to the result where it is all of a group, else to the partial sums
+__device__ __forceinline__ bool weight_span(const WeightArgs &p, int index, Span *s, Sink *sink)
+{
+    int64_t at;
+    *sink = p.sink;
+    if (p.step) {
+        if (!find_piece(p.ptr, p.n_groups, p.n_rows, p.step, index, s)) return false;
+        int32_t lo, hi;
+        group_range(p.ptr, s->group, p.n_groups, p.n_rows, &lo, &hi);
+        at = s->group;
+        if (hi - lo > p.step) {
+            *sink = Sink{p.part, p.sink.ld, nullptr, p.sink.n_cols, 0, 0, 0};
+            at = index;
+        }
+    } else {
+        s->group = index;
+        group_range(p.ptr, index, p.n_groups, p.n_rows, &s->row, &s->end);
+        at = index;
+    }
+    sink->out = static_cast<char *>(sink->out) + at * p.d_in * p.d_out * (sink->bf16 ? 2 : 4);
+    return true;
+}
+
+// weights' gradient: tiles of [d_in x d_out] per group, or per piece of `step` rows (joined by sum_pieces_kernel)
 template <typename T, Kind KIND, bool ODD>
 __global__ __launch_bounds__(kind_threads(KIND)) __attribute__((amdgpu_waves_per_eu(2))) void grouped_weight_kernel(const WeightArgs p)
 {
@@ -624,12 +665,8 @@ __global__ __launch_bounds__(kind_threads(KIND)) __attribute__((amdgpu_waves_per
     __shared__ __attribute__((aligned(16))) char lds[2 * K::kStage];
     const int tiles = p.row_tiles * p.col_tiles, index = static_cast<int>(blockIdx.x) / tiles;
     Span s;
-    if (p.step) {
-        if (!find_piece(p.ptr, p.n_groups, p.n_rows, p.step, index, &s)) return;
-    } else {
-        s.group = index;
-        group_range(p.ptr, s.group, p.n_groups, p.n_rows, &s.row, &s.end);
-    }
+    Sink sink;
+    if (!weight_span(p, index, &s, &sink)) return;
     int row, col;
     band_order(static_cast<int>(blockIdx.x) % tiles, p.row_tiles, p.col_tiles, kBandRows / BM, &row, &col);
     const int row0 = row * BM, col0 = col * BN;
@@ -641,9 +678,6 @@ __global__ __launch_bounds__(kind_threads(KIND)) __attribute__((amdgpu_waves_per
     b.ld = p.ld_dz; b.rows = p.d_out - col0; b.col0 = col0; b.depth = a.depth;
     typename K::Acc acc;
     run_kind<K, KIND>(a, b, lds, acc);
-    Sink sink = p.sink;
-    const int64_t first = static_cast<int64_t>(index) * p.d_in;
-    sink.out = static_cast<char *>(sink.out) + first * p.d_out * (sink.bf16 ? 2 : 4);
     K::put(sink, acc, row0, p.d_in, col0);
 }
 
@@ -687,63 +721,72 @@ __global__ __launch_bounds__(256) void tiny_weight_kernel(const WeightArgs p)
 {
     const int tiles = p.row_tiles * p.col_tiles, index = static_cast<int>(blockIdx.x) / tiles;
     Span s;
-    if (p.step) {
-        if (!find_piece(p.ptr, p.n_groups, p.n_rows, p.step, index, &s)) return;
-    } else {
-        s.group = index;
-        group_range(p.ptr, s.group, p.n_groups, p.n_rows, &s.row, &s.end);
-    }
+    Sink sink;
+    if (!weight_span(p, index, &s, &sink)) return;
     const int64_t e = static_cast<int64_t>(blockIdx.x % tiles) * 256 + threadIdx.x;
     if (e >= static_cast<int64_t>(p.d_in) * p.d_out) return;
     const int k = static_cast<int>(e / p.d_out), n = static_cast<int>(e % p.d_out);
     float sum = 0.f;
     for (int64_t r = s.row; r < s.end; ++r) sum += to_f32(static_cast<const T *>(p.a)[r * p.ld_a + k]) * to_f32(static_cast<const T *>(p.dz)[r * p.ld_dz + n]);
-    Sink sink = p.sink;
-    sink.out = static_cast<char *>(sink.out) + static_cast<int64_t>(index) * p.d_in * p.d_out * (sink.bf16 ? 2 : 4);
     put1(sink, sum, k, n);
 }
 
-// out[g] (+)= the sum of the partial sums of the group's pieces, `width` values each: a wavefront adds up a quarter of them, front to back
+// out[g] (+)= the sum of the partial sums of the group's pieces, `width` values each: a wavefront adds up a sixteenth of them, front to
+// back.  `whole`: what a group of one piece has is in `out` already.
+constexpr int kJoinWaves = 16;
 struct JoinArgs {
     const float *part;
     const int64_t *ptr;
     void *out;
     int64_t n_rows, width;
-    int32_t n_groups, step, most, bf16, add;
+    int32_t n_groups, step, most, bf16, add, whole;
 };
-__global__ __launch_bounds__(256) void sum_pieces_kernel(const JoinArgs p)
+__global__ __launch_bounds__(64 * kJoinWaves) void sum_pieces_kernel(const JoinArgs p)
 {
-    __shared__ float joined[4][64];
+    __shared__ float joined[kJoinWaves][64];
     const int g = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int32_t lo, hi;
     group_range(p.ptr, g, p.n_groups, p.n_rows, &lo, &hi);
+    const int64_t base = static_cast<int64_t>(g) * p.width;
+    if (lo == hi) {
+        if (p.add) return;
+        for (int64_t c = static_cast<int64_t>(blockIdx.x) * 64 * kJoinWaves + threadIdx.x; c < p.width; c += static_cast<int64_t>(gridDim.x) * 64 * kJoinWaves) {
+            if (p.bf16) static_cast<Bf16 *>(p.out)[base + c].bits = 0;
+            else static_cast<float *>(p.out)[base + c] = 0.f;
+        }
+        return;
+    }
+    if (p.whole && hi - lo <= p.step) return;
     // (overlapping groups could have more pieces than there is room for)
     const int first = count_pieces(p.ptr, g, p.n_rows, p.step, p.most), count = min(pieces_in(hi - lo, p.step), p.most - first);
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * 64 + lane;
-    float sum = 0.f;
-    if (c < p.width) {
-        const int to = (wave + 1) * count / 4;
+    for (int64_t c0 = static_cast<int64_t>(blockIdx.x) * 64; c0 < p.width; c0 += static_cast<int64_t>(gridDim.x) * 64) {
+        const int64_t c = c0 + lane;
+        float sum = 0.f;
+        if (c < p.width) {
+            const int to = (wave + 1) * count / kJoinWaves;
 #pragma unroll 8
-        for (int i = wave * count / 4; i < to; ++i) sum += p.part[(first + i) * p.width + c];
+            for (int i = wave * count / kJoinWaves; i < to; ++i) sum += p.part[(first + i) * p.width + c];
+        }
+        joined[wave][lane] = sum;
+        __syncthreads();
+        if (wave == 0 && c < p.width) {
+#pragma unroll
+            for (int w = 1; w < kJoinWaves; ++w) sum += joined[w][lane];
+            if (p.bf16) { Bf16 *o = static_cast<Bf16 *>(p.out) + base + c; from_f32(sum + (p.add ? to_f32(*o) : 0.f), *o); }
+            else { float *o = static_cast<float *>(p.out) + base + c; *o = sum + (p.add ? *o : 0.f); }
+        }
+        __syncthreads();
     }
-    joined[wave][lane] = sum;
-    __syncthreads();
-    if (wave != 0 || c >= p.width) return;
-    sum = joined[0][lane] + joined[1][lane] + joined[2][lane] + joined[3][lane];
-    const int64_t at = static_cast<int64_t>(g) * p.width + c;
-    if (p.bf16) { Bf16 *o = static_cast<Bf16 *>(p.out) + at; from_f32(sum + (p.add ? to_f32(*o) : 0.f), *o); }
-    else { float *o = static_cast<float *>(p.out) + at; *o = sum + (p.add ? *o : 0.f); }
 }
 
 // dz = grad_out where out > 0 (RELU; written for the two products), and its column sums over pieces of rows.  Bound by HBM.
-constexpr int kMaskRows = 128;
 struct MaskArgs {
     const void *grad, *out;
     void *dz;               // NULL: grad is dz already
     float *part;            // NULL: no column sums
     const int64_t *ptr;
     int64_t n_rows, ld_grad, ld_out, ld_dz;
-    int32_t n_groups, d_out, out_bf16, lanes_log2;
+    int32_t n_groups, d_out, out_bf16, lanes_log2, step;
 };
 // 2^lanes_log2 lanes take a row, V columns each; a wavefront 64 / 2^lanes_log2 rows at a time
 template <typename T, int V>
@@ -751,7 +794,7 @@ __global__ __launch_bounds__(256) void mask_rows_kernel(const MaskArgs p)
 {
     __shared__ float joined[256 * V];
     Span s;
-    if (!find_piece(p.ptr, p.n_groups, p.n_rows, kMaskRows, static_cast<int>(blockIdx.x), &s)) return;
+    if (!find_piece(p.ptr, p.n_groups, p.n_rows, p.step, static_cast<int>(blockIdx.x), &s)) return;
     const int lanes = 1 << p.lanes_log2, groups = 256 >> p.lanes_log2, group = threadIdx.x >> p.lanes_log2;
     const int64_t c = ((static_cast<int64_t>(blockIdx.y) << p.lanes_log2) + (threadIdx.x & (lanes - 1))) * V;
     const int64_t col = c + V <= p.d_out ? c : p.d_out - V;         // the last vector ends with the row; the columns before c are its neighbour's
@@ -811,6 +854,7 @@ struct GradPlan {
     int32_t step;                   // rows of a piece of the weights' gradient, 0: groups whole
     int64_t row_tiles, col_tiles;
     int64_t pieces, mask_pieces;    // at most
+    int32_t mask_step;
     int64_t ld_dz;
     size_t dz, part, bias_part, bytes;
 };
@@ -821,7 +865,7 @@ GradPlan plan_grad(int64_t n_rows, int32_t n_groups, int32_t d_in, int32_t d_out
     const int32_t chunk = dtype == MGG_BF16 ? 8 : 4;
     const int64_t present = n_groups < n_rows ? n_groups : n_rows;      // groups that can have rows
     g.tiny = d_in < chunk || d_out < chunk;
-    g.kind = d_out > 64 ? MEDIUM : (d_in > 64 ? NARROW : SMALL);
+    g.kind = dtype == MGG_F32 || (d_in <= 64 && d_out <= 64) ? SMALL : (d_out > 64 ? MEDIUM : NARROW);
     if (dtype == MGG_BF16 && g.kind == MEDIUM && d_in % chunk == 0 && d_out % chunk == 0 &&
         large_pays(n_groups * ceil_div(d_in, 256) * ceil_div(d_out, 256), n_groups * ceil_div(d_in, 128) * ceil_div(d_out, 128)))
         g.kind = LARGE;
@@ -835,7 +879,10 @@ GradPlan plan_grad(int64_t n_rows, int32_t n_groups, int32_t d_in, int32_t d_out
         g.step = static_cast<int32_t>(step < 256 ? 256 : (step < (1 << 30) ? step : 1 << 30));
         g.pieces = n_rows / g.step + present;
     }
-    g.mask_pieces = n_rows / kMaskRows + present;
+    // some 2048 blocks of the mask, 64 rows and 64 x 16 bytes at least
+    g.mask_step = static_cast<int32_t>(ceil_div(ceil_div(n_rows * ceil_div(d_out, 64 * chunk), 2048), 64) * 64);
+    if (g.mask_step < 64) g.mask_step = 64;
+    g.mask_pieces = n_rows / g.mask_step + present;
     g.ld_dz = static_cast<int64_t>(round_up(static_cast<size_t>(d_out), 8));
     size_t at = 0;
     g.dz = at; at += relu ? round_up(static_cast<size_t>(n_rows) * g.ld_dz * (dtype == MGG_BF16 ? 2 : 4), 256) : 0;
@@ -875,9 +922,11 @@ mgg_status_t rows_product(RowsArgs p, hipStream_t stream)
     }
     // few rows to a group: reading the weights is what takes the time
     if (p.n_rows <= 24 * static_cast<int64_t>(p.n_groups) || p.n_rows <= 64) {
+        // (8 wavefronts where blocks are few; 64 rows over 64 groups 1024 -> 2048 with 4: 40 us, with 8: 50; one row 4096 -> 4096 with
+        // 8: 23 us, with 4: 27, as its 64 blocks fill a quarter of the chip)
         MGG_GRID(32, 64);
-        if (blocks < 2 * kCus) hipLaunchKernelGGL((grouped_few_rows_kernel<T, 8, B_ALONG, ODD>), blocks_dim, dim3(512), 0, stream, p);
-        else hipLaunchKernelGGL((grouped_few_rows_kernel<T, 4, B_ALONG, ODD>), blocks_dim, dim3(256), 0, stream, p);
+        if (blocks < 2 * kCus) hipLaunchKernelGGL((grouped_few_rows_kernel<T, 64, 8, B_ALONG, ODD>), blocks_dim, dim3(512), 0, stream, p);
+        else hipLaunchKernelGGL((grouped_few_rows_kernel<T, 64, 4, B_ALONG, ODD>), blocks_dim, dim3(256), 0, stream, p);
         return launched("grouped product launch");
     }
     if constexpr (!ODD && sizeof(T) == 2) {
@@ -888,7 +937,11 @@ mgg_status_t rows_product(RowsArgs p, hipStream_t stream)
             return launched("grouped product launch");
         }
     }
-    if (cols <= 64) {
+    if constexpr (sizeof(T) == 4) {
+        MGG_GRID(64, 64);
+        hipLaunchKernelGGL((grouped_rows_kernel<T, SMALL, B_ALONG, ODD>), blocks_dim, dim3(256), 0, stream, p);
+        return launched("grouped product launch");
+    } else if (cols <= 64) {
         MGG_GRID(128, 64);
         hipLaunchKernelGGL((grouped_rows_kernel<T, NARROW, B_ALONG, ODD>), blocks_dim, dim3(256), 0, stream, p);
     } else {
@@ -915,10 +968,12 @@ mgg_status_t weight_product(WeightArgs p, const GradPlan &g, hipStream_t stream)
     if (g.row_tiles > INT32_MAX || g.pieces * g.row_tiles > INT32_MAX / g.col_tiles) return fail(MGG_ERR_UNSUPPORTED, "too many tiles for one launch");
     const dim3 grid(static_cast<unsigned>(g.pieces * g.row_tiles * g.col_tiles));
     if (g.tiny) hipLaunchKernelGGL((tiny_weight_kernel<T>), grid, dim3(256), 0, stream, p);
-    else if (g.kind == MEDIUM) hipLaunchKernelGGL((grouped_weight_kernel<T, MEDIUM, ODD>), grid, dim3(256), 0, stream, p);
-    else if (g.kind == NARROW) hipLaunchKernelGGL((grouped_weight_kernel<T, NARROW, ODD>), grid, dim3(256), 0, stream, p);
     else if (g.kind == SMALL) hipLaunchKernelGGL((grouped_weight_kernel<T, SMALL, ODD>), grid, dim3(256), 0, stream, p);
-    else if constexpr (!ODD && sizeof(T) == 2) hipLaunchKernelGGL((grouped_weight_kernel<T, LARGE, ODD>), grid, dim3(512), 0, stream, p);
+    else if constexpr (sizeof(T) == 2) {
+        if (g.kind == MEDIUM) hipLaunchKernelGGL((grouped_weight_kernel<T, MEDIUM, ODD>), grid, dim3(256), 0, stream, p);
+        else if (g.kind == NARROW) hipLaunchKernelGGL((grouped_weight_kernel<T, NARROW, ODD>), grid, dim3(256), 0, stream, p);
+        else if constexpr (!ODD) hipLaunchKernelGGL((grouped_weight_kernel<T, LARGE, ODD>), grid, dim3(512), 0, stream, p);
+    }
     return launched("grouped weight gradient launch");
 }
 
@@ -930,9 +985,8 @@ mgg_status_t weight_product_of(const WeightArgs &p, const GradPlan &g, hipStream
 
 mgg_status_t join_pieces(const JoinArgs &p, hipStream_t stream)
 {
-    const int64_t blocks = ceil_div(p.width, 64);
-    if (blocks > INT32_MAX) return fail(MGG_ERR_UNSUPPORTED, "too many columns for one launch");
-    hipLaunchKernelGGL(sum_pieces_kernel, dim3(static_cast<unsigned>(blocks), p.n_groups), dim3(256), 0, stream, p);
+    const int64_t columns = ceil_div(p.width, 64), some = 8192 / p.n_groups + 1;
+    hipLaunchKernelGGL(sum_pieces_kernel, dim3(static_cast<unsigned>(columns < some ? columns : some), p.n_groups), dim3(64 * kJoinWaves), 0, stream, p);
     return launched("partial sum launch");
 }
 
@@ -977,7 +1031,7 @@ mgg_status_t launch_update_grouped_grad(const GroupedGrad &q, void *workspace, h
     mgg_status_t s = MGG_OK;
     if (q.n_rows > 0 && (q.grad_bias || (q.relu && (q.grad_a || q.grad_w)))) {
         MaskArgs m{};
-        m.grad = q.grad_out; m.ptr = q.group_ptr; m.n_rows = q.n_rows; m.ld_grad = q.ld_grad; m.n_groups = q.n_groups; m.d_out = q.d_out;
+        m.grad = q.grad_out; m.ptr = q.group_ptr; m.n_rows = q.n_rows; m.ld_grad = q.ld_grad; m.n_groups = q.n_groups; m.d_out = q.d_out; m.step = g.mask_step;
         if (q.relu) {
             m.out = q.out; m.ld_out = q.ld_out; m.out_bf16 = q.out_dtype == MGG_BF16;
             if (q.grad_a || q.grad_w) { m.dz = ws + g.dz; m.ld_dz = g.ld_dz; dz = m.dz; ld_dz = m.ld_dz; }
@@ -987,8 +1041,8 @@ mgg_status_t launch_update_grouped_grad(const GroupedGrad &q, void *workspace, h
         if (s != MGG_OK) return s;
     }
     if (q.grad_bias) {
-        s = join_pieces(JoinArgs{reinterpret_cast<float *>(ws + g.bias_part), q.group_ptr, q.grad_bias, q.n_rows, q.d_out, q.n_groups, kMaskRows,
-                                 static_cast<int32_t>(g.mask_pieces), 0, q.add_bias}, stream);
+        s = join_pieces(JoinArgs{reinterpret_cast<float *>(ws + g.bias_part), q.group_ptr, q.grad_bias, q.n_rows, q.d_out, q.n_groups, g.mask_step,
+                                 static_cast<int32_t>(g.mask_pieces), 0, q.add_bias, 0}, stream);
         if (s != MGG_OK) return s;
     }
     if (q.grad_a) {
@@ -1003,12 +1057,12 @@ mgg_status_t launch_update_grouped_grad(const GroupedGrad &q, void *workspace, h
         WeightArgs p{};
         p.a = q.a; p.dz = dz; p.ptr = q.group_ptr; p.n_rows = q.n_rows; p.ld_a = q.ld_a; p.ld_dz = ld_dz;
         p.n_groups = q.n_groups; p.d_in = q.d_in; p.d_out = q.d_out; p.step = g.step;
-        if (g.step) p.sink = Sink{ws + g.part, q.d_out, nullptr, q.d_out, 0, 0, 0};
-        else p.sink = Sink{q.grad_w, q.d_out, nullptr, q.d_out, q.grad_w_dtype == MGG_BF16, 0, q.add_w};
+        p.sink = Sink{q.grad_w, q.d_out, nullptr, q.d_out, q.grad_w_dtype == MGG_BF16, 0, q.add_w};
+        p.part = reinterpret_cast<float *>(ws + g.part);
         s = bf16 ? weight_product_of<Bf16>(p, g, stream) : weight_product_of<float>(p, g, stream);
         if (s != MGG_OK || !g.step) return s;
         s = join_pieces(JoinArgs{reinterpret_cast<float *>(ws + g.part), q.group_ptr, q.grad_w, q.n_rows, static_cast<int64_t>(q.d_in) * q.d_out, q.n_groups, g.step,
-                                 static_cast<int32_t>(g.pieces), q.grad_w_dtype == MGG_BF16, q.add_w}, stream);
+                                 static_cast<int32_t>(g.pieces), q.grad_w_dtype == MGG_BF16, q.add_w, 1}, stream);
     }
     return s;
 }
