@@ -106,7 +106,7 @@ _lib = None
 
 def lib():
     """Load libmgg.so (built in-tree by ``paper_2209_06800_amd.build``); raises if absent."""
-    global _lib
+    global _lib, _current_device
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise ImportError(f"{LIB_PATH} is missing: run `python -m paper_2209_06800_amd.build` "
@@ -116,6 +116,7 @@ def lib():
         import torch
         _DTYPE_CODE.update({torch.float32: F32, torch.bfloat16: BF16})
         _INDEX_CODE.update({torch.int32: I32, torch.int64: I64})
+        _current_device = torch.cuda.current_device
         L = C.CDLL(LIB_PATH)
         L.mgg_last_error.restype = C.c_char_p
         L.mgg_version.restype = C.c_char_p
@@ -216,6 +217,7 @@ _DTYPE_CODE = {}                # torch dtype -> mgg_dtype_t, filled when the li
 
 
 _INDEX_CODE = {}                # the same for mgg_index_t
+_current_device = None     # torch's getter of the current device's number
 
 
 def _torch_dtype_code(t) -> int:
@@ -589,20 +591,17 @@ def mgg_layer_forward(part: Partition, mode: str, x_local, x_halo, weights, acts
 # Lookup, grouped Update and distillation loss.  What the C ABI cannot see is checked here: shapes, dtypes, and that every
 # tensor lives on the current device (whose stream the call goes to).
 def _same_device(*tensors):
-    import torch
-    device = None
+    lib()                       # (torch is there from here on)
+    first = tensors[0].get_device()
     for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise TypeError("device tensor expected")
-        if device is None:
-            device = t.device
-            if device.index != torch.cuda.current_device():
-                raise ValueError(f"tensors live on {device}, the current device is cuda:{torch.cuda.current_device()}")
-        elif t.device != device:
-            raise ValueError(f"tensors live on {device} and on {t.device}")
-    return device
+        if t is not None:
+            index = t.get_device()
+            if index < 0:
+                raise TypeError("device tensor expected")
+            if index != first:
+                raise ValueError(f"tensors live on cuda:{first} and on cuda:{index}")
+    if first != _current_device():
+        raise ValueError(f"tensors live on cuda:{first}, the current device is cuda:{_current_device()}")
 
 
 def _code(dtype) -> int:
@@ -621,31 +620,31 @@ def _index_code(t) -> int:
     return code
 
 
-def _new(shape, dtype, device, stream):
+def _new(shape, dtype, like, stream):
     """A tensor that belongs to the stream the call goes to: memory freed there is not given to work on another one."""
-    import torch
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
-
-
-def _workspace(workspace, need: int, device, stream):
+        return like.new_empty(shape, dtype=dtype)
     import torch
+    with torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
+
+
+def _workspace(workspace, need: int, like, stream):
     if workspace is None:
-        return _new((max(need, 1),), torch.uint8, device, stream)
+        import torch
+        return _new((max(need, 1),), torch.uint8, like, stream)
     if not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
     return workspace
 
 
 def _shape(name: str, t, rows: int, cols: int):
-    if t is not None and (t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols):
+    if t is not None and t.shape != (rows, cols):
         raise ValueError(f"{name} must be {rows} x {cols}, got {tuple(t.shape)}")
 
 
 def _ids_1d(ids):
-    if ids.dim() != 1 or (ids.shape[0] > 1 and ids.stride(0) != 1):
+    if ids.dim() != 1 or not ids.is_contiguous():
         raise ValueError("ids must be a contiguous 1-D tensor")
     return _index_code(ids)
 
@@ -654,11 +653,13 @@ def mgg_embed(ids, table, *, scale: float = 1.0, out=None, out_dtype=None, strea
     """out[i] = scale * table[ids[i]]; an id outside the table (padding) gives a row of zeros.  The output has the table's
     dtype unless `out` or `out_dtype` says otherwise."""
     id_type = _ids_1d(ids)
-    n, rows, dim = int(ids.shape[0]), int(table.shape[0]), int(table.shape[1])
-    device = _same_device(ids, table, out)
+    n = ids.shape[0]
+    rows, dim = table.shape
+    _same_device(ids, table, out)
     if out is None:
-        out = _new((n, dim), out_dtype or table.dtype, device, stream)
-    _shape("out", out, n, dim)
+        out = _new((n, dim), out_dtype or table.dtype, table, stream)
+    else:
+        _shape("out", out, n, dim)
     _check(lib().mgg_embed(n, id_type, ids.data_ptr(), rows, _code(table.dtype), table.data_ptr(), dim, _ld(table), scale, _code(out.dtype),
                            out.data_ptr(), _ld(out), _stream(stream)))
     return out
@@ -676,13 +677,13 @@ def mgg_embed_grad(ids, grad_out, table_rows: int, *, scale: float = 1.0, out=No
     id_type = _ids_1d(ids)
     n, dim = int(ids.shape[0]), int(grad_out.shape[1])
     _shape("grad_out", grad_out, n, dim)
-    device = _same_device(ids, grad_out, out, workspace)
+    _same_device(ids, grad_out, out, workspace)
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs `out`")
-        out = _new((table_rows, dim), out_dtype or torch.float32, device, stream)
+        out = _new((table_rows, dim), out_dtype or torch.float32, grad_out, stream)
     _shape("out", out, table_rows, dim)
-    workspace = _workspace(workspace, mgg_embed_grad_workspace_bytes(n, table_rows, dim), device, stream)
+    workspace = _workspace(workspace, mgg_embed_grad_workspace_bytes(n, table_rows, dim), grad_out, stream)
     _check(lib().mgg_embed_grad(n, id_type, ids.data_ptr(), table_rows, _code(grad_out.dtype), grad_out.data_ptr(), dim, _ld(grad_out), scale,
                                 int(accumulate), _code(out.dtype), out.data_ptr(), _ld(out), workspace.data_ptr(),
                                 workspace.numel() * workspace.element_size(), _stream(stream)))
@@ -711,9 +712,9 @@ def mgg_update_grouped(group_ptr, a, w, bias=None, act: str = "none", *, out=Non
     n, d_in, d_out = int(a.shape[0]), int(w.shape[1]), int(w.shape[2])
     _shape("a", a, n, d_in)
     _check_bias("bias", bias, n_groups, d_out)
-    device = _same_device(group_ptr, a, w, bias, out)
+    _same_device(group_ptr, a, w, bias, out)
     if out is None:
-        out = _new((n, d_out), out_dtype or a.dtype, device, stream)
+        out = _new((n, d_out), out_dtype or a.dtype, a, stream)
     _shape("out", out, n, d_out)
     _check(lib().mgg_update_grouped(n, n_groups, group_ptr.data_ptr(), _code(a.dtype), a.data_ptr(), _ld(a), d_in, _code(w.dtype), w.data_ptr(),
                                     _dev_ptr(bias), d_out, _ACT[act], _code(out.dtype), out.data_ptr(), _ld(out), _stream(stream)))
@@ -741,20 +742,20 @@ def mgg_update_grouped_grad(group_ptr, grad_out, a, w, act: str = "none", *, out
         raise ValueError("the gradient of a ReLU needs the forward call's `out`")
     if act == "relu":
         _shape("out", out, n, d_out)
-    device = _same_device(group_ptr, grad_out, a, w, out if act == "relu" else None, grad_a, grad_w, grad_bias, workspace)
+    _same_device(group_ptr, grad_out, a, w, out if act == "relu" else None, grad_a, grad_w, grad_bias, workspace)
     add = (ACC_W if accumulate and grad_w is not None else 0) | (ACC_BIAS if accumulate and grad_bias is not None else 0)
     if need_a and grad_a is None:
-        grad_a = _new((n, d_in), a.dtype, device, stream)
+        grad_a = _new((n, d_in), a.dtype, a, stream)
     if need_w and grad_w is None:
-        grad_w = _new((n_groups, d_in, d_out), w_grad_dtype or torch.float32, device, stream)
+        grad_w = _new((n_groups, d_in, d_out), w_grad_dtype or torch.float32, a, stream)
     if need_bias and grad_bias is None:
-        grad_bias = _new((n_groups, d_out), torch.float32, device, stream)
+        grad_bias = _new((n_groups, d_out), torch.float32, a, stream)
     _shape("grad_a", grad_a, n, d_in)
     if grad_w is not None and (tuple(grad_w.shape) != tuple(w.shape) or not grad_w.is_contiguous()):
         raise ValueError(f"grad_w must be contiguous and {tuple(w.shape)}, got {tuple(grad_w.shape)}")
     _check_bias("grad_bias", grad_bias, n_groups, d_out)
     relu_out = out if act == "relu" else None
-    workspace = _workspace(workspace, mgg_update_grouped_grad_workspace_bytes(n, n_groups, d_in, d_out, w.dtype, act=act), device, stream)
+    workspace = _workspace(workspace, mgg_update_grouped_grad_workspace_bytes(n, n_groups, d_in, d_out, w.dtype, act=act), a, stream)
     _check(lib().mgg_update_grouped_grad(
         n, n_groups, group_ptr.data_ptr(), _code(w.dtype), grad_out.data_ptr(), _ld(grad_out), _ACT[act],
         F32 if relu_out is None else _code(relu_out.dtype), _dev_ptr(relu_out), 0 if relu_out is None else _ld(relu_out), a.data_ptr(), _ld(a), d_in,
@@ -782,13 +783,13 @@ def mgg_distill_loss(logits, top_ids, top_logits, *, temperature: float = 1.0, r
         raise ValueError(f"row_weight must be a contiguous fp32 tensor of {n} values")
     if loss is not None and (loss.dtype != torch.float32 or tuple(loss.shape) != (n,) or not loss.is_contiguous()):
         raise ValueError(f"loss must be a contiguous fp32 tensor of {n} values")
-    device = _same_device(logits, top_ids, top_logits, row_weight, grad, loss, workspace)
+    _same_device(logits, top_ids, top_logits, row_weight, grad, loss, workspace)
     if loss is None:
-        loss = _new((n,), torch.float32, device, stream)
+        loss = _new((n,), torch.float32, logits, stream)
     if grad is None and need_grad:
-        grad = _new((n, classes), grad_dtype or logits.dtype, device, stream)
+        grad = _new((n, classes), grad_dtype or logits.dtype, logits, stream)
     _shape("grad", grad, n, classes)
-    workspace = _workspace(workspace, mgg_distill_workspace_bytes(n, classes), device, stream)
+    workspace = _workspace(workspace, mgg_distill_workspace_bytes(n, classes), logits, stream)
     _check(lib().mgg_distill_loss(n, classes, _code(logits.dtype), logits.data_ptr(), _ld(logits), k, id_type, top_ids.data_ptr(), _ld(top_ids),
                                   _code(top_logits.dtype), top_logits.data_ptr(), _ld(top_logits), temperature, _dev_ptr(row_weight), loss.data_ptr(),
                                   F32 if grad is None else _code(grad.dtype), _dev_ptr(grad), 0 if grad is None else _ld(grad), workspace.data_ptr(),

@@ -268,20 +268,21 @@ struct Sink {
     int32_t bf16, relu, add;
 };
 
-template <typename Out>
-__device__ __forceinline__ void put8(Out *o, float (&v)[8], int cols, bool add)
+// the first `cols` of N values to o, on top of what is there where `add` says so
+template <int N, typename Out>
+__device__ __forceinline__ void put_cols(Out *o, float (&v)[N], int cols, bool add)
 {
-    if (cols >= 8) {
+    if (cols >= N) {
         if (add) {
-            float old[8];
-            load_n<8>(o, old);
+            float old[N];
+            load_n<N>(o, old);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += old[e];
+            for (int e = 0; e < N; ++e) v[e] += old[e];
         }
-        store_n<8>(o, v);
+        store_n<N>(o, v);
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
+        for (int e = 0; e < N; ++e)
             if (e < cols) from_f32(v[e] + (add ? to_f32(o[e]) : 0.f), o[e]);
     }
 }
@@ -316,8 +317,8 @@ __device__ __forceinline__ void put_tile(const Sink &p, const f32x16 &acc, int64
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = v[e] < 0.f ? 0.f : v[e];
         }
-        if (p.bf16) put8(static_cast<Bf16 *>(p.out) + r * p.ld + col, v, p.n_cols - col, p.add);
-        else put8(static_cast<float *>(p.out) + r * p.ld + col, v, p.n_cols - col, p.add);
+        if (p.bf16) put_cols<8>(static_cast<Bf16 *>(p.out) + r * p.ld + col, v, p.n_cols - col, p.add);
+        else put_cols<8>(static_cast<float *>(p.out) + r * p.ld + col, v, p.n_cols - col, p.add);
     }
 }
 
@@ -731,9 +732,9 @@ __global__ __launch_bounds__(256) void tiny_weight_kernel(const WeightArgs p)
     put1(sink, sum, k, n);
 }
 
-// out[g] (+)= the sum of the partial sums of the group's pieces, `width` values each: a wavefront adds up a sixteenth of them, front to
-// back.  `whole`: what a group of one piece has is in `out` already.
-constexpr int kJoinWaves = 16;
+// out[g] (+)= the sum of the partial sums of the group's pieces, `width` values each: the wavefronts of a block share them,
+// each front to back.  `whole`: what a group of one piece has is in `out` already.
+constexpr int kJoinWaves = 16, kJoinCols = 4;
 struct JoinArgs {
     const float *part;
     const int64_t *ptr;
@@ -741,9 +742,21 @@ struct JoinArgs {
     int64_t n_rows, width;
     int32_t n_groups, step, most, bf16, add, whole;
 };
+// the values of columns [col, col + kJoinCols), those from c on
+template <typename Out>
+__device__ __forceinline__ void put_own(Out *row, float (&v)[kJoinCols], int64_t c, int64_t col, int64_t width, bool add)
+{
+    if (c == col && c + kJoinCols <= width) {
+        put_cols<kJoinCols>(row + c, v, kJoinCols, add);
+    } else {
+#pragma unroll
+        for (int e = 0; e < kJoinCols; ++e)
+            if (col + e >= c && col + e < width) from_f32(v[e] + (add ? to_f32(row[col + e]) : 0.f), row[col + e]);
+    }
+}
 __global__ __launch_bounds__(64 * kJoinWaves) void sum_pieces_kernel(const JoinArgs p)
 {
-    __shared__ float joined[kJoinWaves][64];
+    __shared__ float joined[kJoinCols][kJoinWaves][64];
     const int g = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int32_t lo, hi;
     group_range(p.ptr, g, p.n_groups, p.n_rows, &lo, &hi);
@@ -759,23 +772,44 @@ __global__ __launch_bounds__(64 * kJoinWaves) void sum_pieces_kernel(const JoinA
     if (p.whole && hi - lo <= p.step) return;
     // (overlapping groups could have more pieces than there is room for)
     const int first = count_pieces(p.ptr, g, p.n_rows, p.step, p.most), count = min(pieces_in(hi - lo, p.step), p.most - first);
-    for (int64_t c0 = static_cast<int64_t>(blockIdx.x) * 64; c0 < p.width; c0 += static_cast<int64_t>(gridDim.x) * 64) {
-        const int64_t c = c0 + lane;
-        float sum = 0.f;
-        if (c < p.width) {
-            const int to = (wave + 1) * count / kJoinWaves;
-#pragma unroll 8
-            for (int i = wave * count / kJoinWaves; i < to; ++i) sum += p.part[(first + i) * p.width + c];
-        }
-        joined[wave][lane] = sum;
-        __syncthreads();
-        if (wave == 0 && c < p.width) {
+    // four pieces at least to a wavefront; the wavefronts that are left take other columns
+    int split = 1;
+    while (split < kJoinWaves && count >= 8 * split) split *= 2;
+    const int share = wave % split, from = share * count / split, to = (share + 1) * count / split;
+    const int64_t block_cols = kJoinWaves / split * 64 * kJoinCols;
+    for (int64_t c0 = static_cast<int64_t>(blockIdx.x) * block_cols; c0 < p.width; c0 += static_cast<int64_t>(gridDim.x) * block_cols) {
+        // (the last columns' vector is moved back to end with the row; what it has of its neighbour's is not written)
+        const int64_t c = c0 + (wave / split * 64 + lane) * kJoinCols, col = max(min(c, p.width - kJoinCols), static_cast<int64_t>(0));
+        float sum[kJoinCols] = {};
+        if (p.width >= kJoinCols) {
+#pragma unroll 4
+            for (int i = from; i < to; ++i) {
+                float x[kJoinCols];
+                load_n<kJoinCols>(p.part + (first + i) * p.width + col, x);
 #pragma unroll
-            for (int w = 1; w < kJoinWaves; ++w) sum += joined[w][lane];
-            if (p.bf16) { Bf16 *o = static_cast<Bf16 *>(p.out) + base + c; from_f32(sum + (p.add ? to_f32(*o) : 0.f), *o); }
-            else { float *o = static_cast<float *>(p.out) + base + c; *o = sum + (p.add ? *o : 0.f); }
+                for (int e = 0; e < kJoinCols; ++e) sum[e] += x[e];
+            }
+        } else {
+#pragma unroll 4
+            for (int i = from; i < to; ++i)
+#pragma unroll
+                for (int e = 0; e < kJoinCols; ++e) sum[e] += p.part[(first + i) * p.width + min(static_cast<int64_t>(e), p.width - 1)];
         }
-        __syncthreads();
+        if (split > 1) {
+#pragma unroll
+            for (int e = 0; e < kJoinCols; ++e) joined[e][wave][lane] = sum[e];
+            __syncthreads();
+            if (share == 0) {
+                for (int w = 1; w < split; ++w)
+#pragma unroll
+                    for (int e = 0; e < kJoinCols; ++e) sum[e] += joined[e][wave + w][lane];
+            }
+        }
+        if (share == 0 && c < p.width) {
+            if (p.bf16) put_own(static_cast<Bf16 *>(p.out) + base, sum, c, col, p.width, p.add);
+            else put_own(static_cast<float *>(p.out) + base, sum, c, col, p.width, p.add);
+        }
+        if (split > 1) __syncthreads();
     }
 }
 
@@ -920,8 +954,11 @@ mgg_status_t rows_product(RowsArgs p, hipStream_t stream)
         hipLaunchKernelGGL((tiny_rows_kernel<T, B_ALONG>), blocks_dim, dim3(256), 0, stream, p);
         return launched("grouped product launch");
     }
-    // few rows to a group: reading the weights is what takes the time
-    if (p.n_rows <= 24 * static_cast<int64_t>(p.n_groups) || p.n_rows <= 64) {
+    // few rows to a group, where reading the weights is what takes the time, or tiles too few to fill the chip, where the depth is
+    // (1500 rows over 2 groups 2048 -> 1024, 104 tiles of 128 x 128: 26 us, with those 41; 2500 rows: 36 and 42; 3000 rows 512 -> 1024, 192
+    // tiles: 19 and 18; fp32 512 rows 2048 -> 1024: 33 and 72)
+    const int64_t tiles = (p.n_rows / 128 + present / 2 + 1) * ceil_div(cols, 128);
+    if (p.n_rows <= 24 * static_cast<int64_t>(p.n_groups) || tiles <= kCus / 2) {
         // (8 wavefronts where blocks are few; 64 rows over 64 groups 1024 -> 2048 with 4: 40 us, with 8: 50; one row 4096 -> 4096 with
         // 8: 23 us, with 4: 27, as its 64 blocks fill a quarter of the chip)
         MGG_GRID(32, 64);
@@ -985,7 +1022,7 @@ mgg_status_t weight_product_of(const WeightArgs &p, const GradPlan &g, hipStream
 
 mgg_status_t join_pieces(const JoinArgs &p, hipStream_t stream)
 {
-    const int64_t columns = ceil_div(p.width, 64), some = 8192 / p.n_groups + 1;
+    const int64_t columns = ceil_div(p.width, 64 * kJoinCols), some = 1024 / p.n_groups + 1;
     hipLaunchKernelGGL(sum_pieces_kernel, dim3(static_cast<unsigned>(columns < some ? columns : some), p.n_groups), dim3(64 * kJoinWaves), 0, stream, p);
     return launched("partial sum launch");
 }
