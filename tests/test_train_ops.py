@@ -213,7 +213,7 @@ def table_grad(ids, grad, rows, scale, into=None):
 
 @gpu
 @pytest.mark.parametrize("n,rows,dim", [(0, 5, 8), (1, 1, 1), (1, 300, 130), (2, 257, 64), (63, 3, 7), (64, 70000, 20), (65, 4, 256), (1000, 5003, 95), (4096, 256, 33),
-                                        (4097, 255, 16), (9000, 40, 602), (20011, 65536, 8), (50000, 1, 24), (100003, 700, 65), (33000, 300000, 4)])
+                                        (4097, 255, 16), (9000, 40, 602), (20011, 65536, 8), (50000, 1, 24), (100003, 700, 65), (33000, 300000, 4), (600001, 3000, 8), (8192, 100000, 16), (8193, 1 << 20, 8)])
 @pytest.mark.parametrize("tin,tout", [(F32, F32), (BF16, F32), (BF16, BF16), (F32, BF16)])
 def test_embed_grad_sums_by_id(n, rows, dim, tin, tout):
     g = torch.Generator().manual_seed(3 * n + rows + dim)
@@ -389,6 +389,49 @@ def test_grouped_gradients(counts, d_in, d_out, dtype, tw, act, accumulate):
         assert all(torch.equal(x, y) for x, y in zip(first, call()))          # the same bits again
 
 
+# Sizes at which the kernels for many rows run: (counts, d_in, d_out, dtype).  Ends inside tiles and inside 16 bytes, empty groups, groups
+# shorter than a tile beside long ones.
+MANY = [
+    ([4000, 0, 1, 4700, 299], 200, 2048, BF16),         # whole chunks: large tiles forward; d_out long: large tiles of the weights' gradient, too
+    ([4000, 0, 1, 4700, 299], 2048, 200, BF16),         # large tiles of the rows' gradient
+    ([64] * 9 + [0, 130, 3] + [70] * 8, 1024, 1032, BF16),
+    ([2500, 7, 2493], 203, 1001, BF16),
+    ([2500, 7, 2493], 1001, 203, BF16),
+    ([12000, 1, 8000], 130, 47, BF16),
+    ([12000, 1, 8000], 48, 136, BF16),
+    ([5000, 0, 4001], 101, 300, F32),
+    ([5000, 0, 4001], 300, 101, F32),
+    ([3000, 200, 2800], 64, 64, BF16),
+    ([257] * 40, 512, 40, F32),
+]
+
+
+@gpu
+@pytest.mark.parametrize("counts,d_in,d_out,dtype", MANY)
+def test_grouped_update_and_gradients_of_many_rows(counts, d_in, d_out, dtype):
+    g = torch.Generator().manual_seed(sum(counts) + d_in + 3 * d_out)
+    n, groups = sum(counts), len(counts)
+    a = torch.randn(n, d_in, generator=g).to(dtype)
+    w = (torch.randn(groups, d_in, d_out, generator=g) * d_in ** -0.5).to(dtype)
+    bias, dz = torch.randn(groups, d_out, generator=g), torch.randn(n, d_out, generator=g).to(dtype)
+    ptr = group_ptr(counts)
+    ref, mag = grouped_reference(ptr, a, w, bias, "relu")
+    out = strided(torch.zeros(n, d_out, dtype=dtype, device=DEV), 3, 1)
+    args = (ptr.to(DEV), a.to(DEV), w.to(DEV), bias.to(DEV), "relu")
+    got = binding.mgg_update_grouped(*args, out=out)
+    assert_within(got, ref, (d_in + 2) * U * mag + half_step(dtype) * ref.abs(), "out")
+    assert int(torch.isnan(out._base).sum()) == out._base.numel() - n * d_out
+    assert torch.equal(binding.mgg_update_grouped(*args), got)
+    masked = torch.where(got.cpu() > 0, dz, torch.zeros((), dtype=dtype))
+    refs, mags = grouped_grad_reference(ptr, masked, a, w)
+    def call():
+        return binding.mgg_update_grouped_grad(args[0], dz.to(DEV), args[1], args[2], "relu", out=got, need_bias=True)
+    grads = call()
+    for name, x, r, m, k in zip(("grad_a", "grad_w", "grad_bias"), grads, refs, mags, (d_out + 2, max(counts) + 3, max(counts) + 3)):
+        assert_within(x, r, k * U * m + half_step(x.dtype) * r.abs(), name)
+    assert all(torch.equal(x, y) for x, y in zip(grads, call()))
+
+
 @gpu
 def test_grouped_gradients_one_at_a_time():
     counts, d_in, d_out = [70, 0, 130], 48, 56
@@ -472,7 +515,7 @@ def draw_distill(n, classes, k, seed, tz, tt, missing=0.1):
 
 @gpu
 @pytest.mark.parametrize("n,classes,k", [(1, 1, 1), (3, 2, 5), (300, 7, 3), (1000, 47, 8), (65, 64, 1), (20, 129, 40), (9, 1000, 64), (5, 4099, 200), (2, 50021, 20),
-                                         (1, 200003, 64), (40, 8200, 16), (3, 33000, 1024), (600, 2051, 4)])
+                                         (1, 200003, 64), (40, 8200, 16), (3, 33000, 1024), (600, 2051, 4), (129, 20001, 7), (128, 70001, 9), (150, 9001, 3)])
 @pytest.mark.parametrize("tz,tt,tg", [(F32, F32, F32), (BF16, F32, BF16), (BF16, BF16, F32), (F32, BF16, BF16)])
 def test_distill_loss_and_gradient(n, classes, k, tz, tt, tg):
     z, ids, top, weight = draw_distill(n, classes, k, n + classes + k, tz, tt)
