@@ -35,13 +35,15 @@ __device__ __forceinline__ void group_range(const int64_t *ptr, int g, int n_gro
     *hi = static_cast<int32_t>(b < *lo ? *lo : (b > n_rows ? n_rows : b));
 }
 
-__device__ __forceinline__ int wave_scan(int v, int lane)
+// inclusive prefix sums over a wavefront, by DPP: within rows of 16 lanes, then the rows' last ones to the rows behind
+__device__ __forceinline__ int wave_scan(int v)
 {
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-        const int o = __shfl_up(v, off);
-        if (lane >= off) v += o;
-    }
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);      // row_shr:1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);     // row_bcast:15 to rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);     // row_bcast:31 to rows 2 and 3
     return v;
 }
 
@@ -50,37 +52,35 @@ __device__ __forceinline__ int pieces_in(int32_t rows, int step) { return rows /
 // pieces of `step` rows in the first n_groups groups, by a wavefront, a group per lane; `most` where overlapping groups would give more
 __device__ __forceinline__ int count_pieces(const int64_t *ptr, int n_groups, int64_t n_rows, int step, int most)
 {
-    int count = 0;
-    for (int g = threadIdx.x & 63; g < n_groups; g += kWave) {
+    int total = 0;
+    for (int g0 = 0; g0 < n_groups; g0 += kWave) {
         int32_t lo, hi;
-        group_range(ptr, g, n_groups, n_rows, &lo, &hi);
-        count = min(count + pieces_in(hi - lo, step), most);
+        group_range(ptr, g0 + (threadIdx.x & 63), n_groups, n_rows, &lo, &hi);
+        total = min(total + min(__builtin_amdgcn_readlane(wave_scan(pieces_in(hi - lo, step)), 63), most), most);
     }
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) count = min(count + __shfl_xor(count, off), most);
-    return __builtin_amdgcn_readfirstlane(count);
+    return total;
 }
 
 // piece number `index`, found by every wavefront for itself, 64 groups at a time
 __device__ __forceinline__ bool find_piece(const int64_t *ptr, int n_groups, int64_t n_rows, int step, int index, Span *s)
 {
-    const int lane = threadIdx.x & 63;
     int before = 0;
     for (int g0 = 0; g0 < n_groups; g0 += kWave) {
         int32_t lo, hi;
-        group_range(ptr, g0 + lane, n_groups, n_rows, &lo, &hi);
-        const int count = pieces_in(hi - lo, step);
-        const int incl = wave_scan(count, lane);
+        group_range(ptr, g0 + (threadIdx.x & 63), n_groups, n_rows, &lo, &hi);
+        const int count = pieces_in(hi - lo, step), incl = wave_scan(count);
         const uint64_t past = __ballot(before + incl > index);
         if (past) {
-            const int at = __ffsll(static_cast<unsigned long long>(past)) - 1;
-            const int first = __shfl(lo, at) + (index - before - __shfl(incl - count, at)) * step, last = __shfl(hi, at);
-            s->group = g0 + __builtin_amdgcn_readfirstlane(at);
-            s->row = __builtin_amdgcn_readfirstlane(first);
-            s->end = __builtin_amdgcn_readfirstlane(last - first < step ? last : first + step);
+            const int at = __builtin_amdgcn_readfirstlane(__ffsll(static_cast<unsigned long long>(past)) - 1);
+            const int first = __builtin_amdgcn_readlane(lo, at) + (index - before - __builtin_amdgcn_readlane(incl - count, at)) * step;
+            const int last = __builtin_amdgcn_readlane(hi, at);
+            if (first < __builtin_amdgcn_readlane(lo, at) || first >= last) return false;       // (sums of overlapping groups can overflow)
+            s->group = g0 + at;
+            s->row = first;
+            s->end = last - first < step ? last : first + step;
             return true;
         }
-        before += __shfl(incl, 63);
+        before += __builtin_amdgcn_readlane(incl, 63);
     }
     return false;
 }
@@ -358,15 +358,18 @@ struct Tile {
 #pragma unroll
             for (int j = 0; j < TN; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j]);
     }
-    static __device__ __forceinline__ void multiply_step(const char *lds, Acc &acc)
+    static __device__ __forceinline__ void multiply_step(const char *lds, Acc &acc, int quarters = 4)
     {
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
+            if (s >= quarters) break;
             Vec16 fa[TM], fb[TN];
             read(lds, s, fa, fb);
             multiply_quarter(fa, fb, acc);
         }
     }
+    // quarters of the last step that hold anything
+    static __device__ __forceinline__ int last_quarters(int depth) { return ((depth - 1) % BK * 4 + BK) / BK; }
     static __device__ __forceinline__ void load(A &a, B &b, int t)
     {
         a.load(t);
@@ -412,7 +415,7 @@ struct Tile {
             multiply_step(lds + (t & 1) * kStage, acc);
             __syncthreads();
         }
-        multiply_step(lds + (t & 1) * kStage, acc);
+        multiply_step(lds + (t & 1) * kStage, acc, last_quarters(a.depth));
     }
 
     // The same for large tiles with two wavefronts on a SIMD, in turns: in every quarter step one of them fetches (its fragments out of LDS,

@@ -414,7 +414,7 @@ struct SumArgs {
     Out *out;
     float *part;
     int64_t n, table_rows, ld_grad, ld_out, ld_part, sum_blocks;
-    int32_t dim, chunk, chunks, lanes_log2, slabs;
+    int32_t dim, chunk, chunks, lanes_log2, slabs, fill_rows;
     float scale;
     int32_t accumulate;
 };
@@ -432,20 +432,20 @@ __device__ __forceinline__ int64_t wave_lower_bound(const uint32_t *a, int64_t l
     return lo + __popcll(__ballot(lo + lane < hi && a[lo + lane] < v));
 }
 
-// which of the 64 ids from `first` on the sorted list has: a bit each.  A step passes 64 keys, or all of the last one's kind.
-__device__ __forceinline__ uint64_t ids_present(const uint32_t *keys, int64_t n, uint32_t first, int lane)
+// which of the `count` (up to 64) ids from `first` on the sorted list has: a bit each.  A step passes 64 keys, or all of the last one's kind.
+__device__ __forceinline__ uint64_t ids_present(const uint32_t *keys, int64_t n, uint32_t first, uint32_t count, int lane)
 {
     uint64_t present = 0;
     int64_t at = wave_lower_bound(keys, 0, n, first, lane);
     while (at < n) {
         const uint32_t key = at + lane < n ? keys[at + lane] : 0xffffffffu;
-        const bool mine = key - first < kWave;
+        const bool mine = key - first < count;
         uint64_t bit = mine ? 1ull << (key - first) : 0ull;
 #pragma unroll
         for (int off = 32; off >= 1; off >>= 1) bit |= __shfl_xor(bit, off);
         present |= bit;
         const uint32_t last = __builtin_amdgcn_readlane(key, 63);
-        if (last - first >= kWave) break;
+        if (last - first >= count) break;
         at = wave_lower_bound(keys, at + kWave, n, last + 1, lane);
     }
     return present;
@@ -481,13 +481,13 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(const SumArgs<In, O
     const int lanes = 1 << p.lanes_log2;
     if (static_cast<int64_t>(blockIdx.x) >= p.sum_blocks) {
         const int lane = threadIdx.x & 63;
-        const int64_t row0 = ((static_cast<int64_t>(blockIdx.x) - p.sum_blocks) * (kThreads / kWave) + (threadIdx.x >> 6)) * kWave;
+        const int64_t row0 = ((static_cast<int64_t>(blockIdx.x) - p.sum_blocks) * (kThreads / kWave) + (threadIdx.x >> 6)) * p.fill_rows;
         if (row0 >= p.table_rows) return;
-        const int64_t left = p.table_rows - row0;
-        const uint64_t rows = ~ids_present(p.keys, p.n, static_cast<uint32_t>(row0), lane) & (left < kWave ? (1ull << left) - 1 : ~0ull);
+        const int count = static_cast<int>(min(p.table_rows - row0, static_cast<int64_t>(p.fill_rows)));
+        const uint64_t rows = ~ids_present(p.keys, p.n, static_cast<uint32_t>(row0), count, lane);
         constexpr int VO = VEC == 1 ? 1 : 16 / static_cast<int>(sizeof(Out));
         const float zero[VO] = {};
-        for (int r = lane >> p.lanes_log2; r < kWave; r += kWave >> p.lanes_log2)
+        for (int r = lane >> p.lanes_log2; r < count; r += kWave >> p.lanes_log2)
             if ((rows >> r) & 1)
                 for (int c = (lane & (lanes - 1)) * VO; c < p.dim; c += lanes * VO)
                     store_n<VO>(p.out + (row0 + r) * p.ld_out + (c + VO <= p.dim ? c : p.dim - VO), zero);
@@ -590,7 +590,10 @@ hipError_t embed_sum(const EmbedGradPlan &s, SumArgs<In, Out> p, hipStream_t str
     p.lanes_log2 = ceil_log2(vecs) < 6 ? ceil_log2(vecs) : 6;
     p.slabs = static_cast<int32_t>(ceil_div(vecs, static_cast<int64_t>(1) << p.lanes_log2));
     p.sum_blocks = ceil_div((s.chunks * p.slabs) << p.lanes_log2, kThreads);
-    const int64_t fill_blocks = p.accumulate ? 0 : ceil_div(p.table_rows, kThreads);
+    // some 32 KB of zeros to a wavefront, up to 64 rows (2 k ids in 5 k rows of 2.4 KB: 64 rows 16 us, 8 rows 8)
+    const int64_t fill = 32768 / (static_cast<int64_t>(p.dim) * static_cast<int64_t>(sizeof(Out)));
+    p.fill_rows = static_cast<int32_t>(fill < 1 ? 1 : (fill < kWave ? fill : kWave));
+    const int64_t fill_blocks = p.accumulate ? 0 : ceil_div(p.table_rows, static_cast<int64_t>(p.fill_rows) * (kThreads / kWave));
     if (p.sum_blocks + fill_blocks > INT32_MAX || s.chunks * p.slabs > INT32_MAX) return hipErrorInvalidConfiguration;
     if (p.sum_blocks + fill_blocks == 0) return hipSuccess;
     hipLaunchKernelGGL((embed_sum_kernel<In, Out, VEC>), dim3(static_cast<unsigned>(p.sum_blocks + fill_blocks)), dim3(kThreads), 0, stream, p);
@@ -631,7 +634,7 @@ mgg_status_t launch_embed_grad(int64_t n, mgg_index_t id_type, const void *ids, 
 #define MGG_SUM(IN, OUT)                                                                                                                                      \
     do {                                                                                                                                                      \
         const SumArgs<IN, OUT> p{keys, pos, static_cast<const IN *>(grad), static_cast<OUT *>(out), reinterpret_cast<float *>(ws + s.part), n, table_rows,       \
-                                 ld_grad, ld_out, s.ld_part, 0, dim, s.chunk, static_cast<int32_t>(s.chunks), 0, 0, scale, accumulate};                         \
+                                 ld_grad, ld_out, s.ld_part, 0, dim, s.chunk, static_cast<int32_t>(s.chunks), 0, 0, 0, scale, accumulate};                         \
         constexpr int VEC = 16 / sizeof(IN);                                                                                                                  \
         e = dim < 8 ? embed_sum<IN, OUT, 1>(s, p, stream) : embed_sum<IN, OUT, VEC>(s, p, stream);                                                              \
     } while (0)

@@ -403,6 +403,9 @@ MANY = [
     ([5000, 0, 4001], 300, 101, F32),
     ([3000, 200, 2800], 64, 64, BF16),
     ([257] * 40, 512, 40, F32),
+    ([9000, 1, 8001], 56, 40, BF16),
+    ([9000, 1, 8001], 47, 33, BF16),
+    ([5000, 0, 4001], 100, 300, F32),
 ]
 
 
