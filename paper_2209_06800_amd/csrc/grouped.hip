@@ -7,6 +7,16 @@
 // An operand along the sum is kept in LDS by rows of 128 bytes and read 16 bytes a lane; one across it is kept by rows of the
 // tile's width, and bf16 is turned on the way out of LDS (ds_read_b64_tr_b16: 16 lanes read 4 rows of 16 elements, a lane gets
 // the four elements of a column).
+//
+// What bounds it and what it reaches (one MI355X; a large library product runs at 1285 TFLOP/s bf16 and 154 fp32, a copy at 5.1 TB/s):
+//   - many rows, bf16: the matrix cores, as far as the clock holds (by the cycle counter 2.0 GHz in launches of 0.3 ms, 1.5 in a run of the one below).  32 k rows over
+//     8 groups 4096 -> 4096: 1.03 - 1.17 ms by the clock, 940 - 1070 TFLOP/s; rows' gradient of 16 k rows 2048 <- 4096:
+//     0.30 ms, weights': 0.28.
+//   - many rows, fp32: the fp32 matrix instruction.  8 k rows 2048 -> 2048 over 4 groups: 0.62 - 0.64 ms, 107 - 111 TFLOP/s.
+//   - few rows to a group: reading the weights.  64 rows over 64 groups 1024 -> 2048 bf16, 41 of them with rows: 38 us, 172 MB at 4.6 TB/s
+//     (30 where the Infinity Cache still holds a part).
+//   - short sums (widths up to some hundred): the chain of a block from its group's offsets over its operands to its stores, a few
+//     microseconds for each of the rounds that fill the chip.  233 k rows 100 -> 256 fp32: 181 - 192 us, where bytes and instructions allow 77.
 #include "train_common.h"
 
 namespace mgg {
@@ -480,7 +490,7 @@ struct Tile {
         store(a, b, lds);
         load(a, b, 1);
         __syncthreads();
-        const bool late = threadIdx.x >= THREADS / 2;
+        const bool late = __builtin_amdgcn_readfirstlane(threadIdx.x) >= THREADS / 2;      // (a scalar: a barrier takes no notice of masked lanes)
         if (late) __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         int t = 0;

