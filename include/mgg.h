@@ -386,7 +386,8 @@ mgg_status_t mgg_layer_forward(const mgg_partition_t *p, const mgg_layer_desc_t 
  * are added to what the rows hold, rows that no id names are not touched.  workspace is a DEVICE buffer of at
  * least mgg_embed_grad_workspace_bytes() bytes, 256-byte aligned, that no other call uses at the same time.
  * Both are asynchronous on `stream`, allocate nothing and can be captured into a graph.
- * Errors: INVALID_ARG, UNSUPPORTED (more than 2^31 - 2 table rows; for the gradient also n beyond 2^30), HIP.
+ * Errors: INVALID_ARG, UNSUPPORTED (more than 2^31 - 2 table rows, n beyond 2^31 - 1, for the gradient beyond 2^30, or so many
+ * short rows that a launch would need 2^32 threads), HIP.  What is refused has written nothing.
  * ------------------------------------------------------------------------------------- */
 typedef enum { MGG_I32 = 0, MGG_I64 = 1 } mgg_index_t;
 
@@ -424,7 +425,8 @@ mgg_status_t mgg_embed_grad(int64_t n, mgg_index_t id_type, const void *ids, int
  * Sums are made in an order that depends on the sizes and group_ptr alone: the same call gives the same bits.
  * Both are asynchronous on `stream`, allocate nothing and can be captured into a graph (group_ptr may change between
  * replays).  Errors: INVALID_ARG, UNSUPPORTED (softmax; a, w and grad_out of two dtypes; more than 2^31 - 1 rows,
- * 2^16 - 1 groups or 2^22 columns or elements from row to row), HIP.
+ * 2^16 - 1 groups or 2^22 columns or elements from row to row, or so many tiles that a launch would need 2^32
+ * threads, which takes 2^30 rows of few columns or 2^32 weights of few columns), HIP.  What is refused has written nothing.
  * ------------------------------------------------------------------------------------- */
 #define MGG_ACC_W 1
 #define MGG_ACC_BIAS 2
@@ -461,7 +463,7 @@ mgg_status_t mgg_update_grouped_grad(int64_t n_rows, int32_t n_groups, const int
  * workspace: a DEVICE buffer of at least mgg_distill_workspace_bytes() bytes, 256-byte aligned, that no other call uses
  * at the same time.  Asynchronous on `stream`, allocates nothing, can be captured into a graph.
  * Errors: INVALID_ARG (a temperature outside [1e-6, 1e6] among them), UNSUPPORTED (k above 1024, 2^31 - 1 classes
- * or rows), HIP.
+ * or rows, or so many rows that a launch would need 2^32 threads: 2^22 rows of 8 k classes and more, 2^30 of a few), HIP.
  * ------------------------------------------------------------------------------------- */
 size_t       mgg_distill_workspace_bytes(int64_t n_rows, int32_t n_classes);   /* 0 on bad arguments */
 mgg_status_t mgg_distill_loss(int64_t n_rows, int32_t n_classes, mgg_dtype_t logits_dtype, const void *logits, int64_t ld_logits,

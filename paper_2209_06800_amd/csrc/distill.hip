@@ -514,27 +514,31 @@ template <typename In, typename Out>
 mgg_status_t launch_typed(DistillArgs p, hipStream_t stream)
 {
     constexpr int N = Vec<In>::N;
+    const char *const refused = "too many rows for one launch";
     const int64_t vecs = ceil_div(p.n_classes, N);
     if (vecs <= kWave * kShortMax) {
         // four lanes at least, which share the teacher's entries; four vectors at most per lane
         p.lanes_log2 = ceil_log2(ceil_div(vecs, kShortMax));
         if (p.lanes_log2 < 2) p.lanes_log2 = 2;
         const int64_t blocks = ceil_div(p.n_rows << p.lanes_log2, kShortThreads), per = ceil_div(vecs, static_cast<int64_t>(1) << p.lanes_log2);
+        if (!launchable(blocks, kShortThreads)) return fail(MGG_ERR_UNSUPPORTED, "%s", refused);
         const dim3 grid(static_cast<unsigned>(blocks));
         if (per <= 1) hipLaunchKernelGGL((distill_short_kernel<In, Out, 1>), grid, dim3(kShortThreads), 0, stream, p);
         else if (per <= 2) hipLaunchKernelGGL((distill_short_kernel<In, Out, 2>), grid, dim3(kShortThreads), 0, stream, p);
         else if (per <= 3) hipLaunchKernelGGL((distill_short_kernel<In, Out, 3>), grid, dim3(kShortThreads), 0, stream, p);
         else hipLaunchKernelGGL((distill_short_kernel<In, Out, 4>), grid, dim3(kShortThreads), 0, stream, p);
     } else if (p.grad && vecs <= 8 * 256) {
+        if (!launchable(p.n_rows, 256)) return fail(MGG_ERR_UNSUPPORTED, "%s", refused);
         launch_rows<In, Out, 256>(p, stream);
     } else if (p.grad && vecs <= 16 * 1024 && (p.n_rows >= 64 || vecs <= 4 * 1024)) {
         // (100 rows of 128 k bf16: 31 us, in pieces 35; 16 rows: 28 and 21; 4 rows of 30 k: 13 and 17)
+        if (!launchable(p.n_rows, 1024)) return fail(MGG_ERR_UNSUPPORTED, "%s", refused);
         launch_rows<In, Out, 1024>(p, stream);
     } else {
         p.pieces = pieces_of(p.n_rows, p.n_classes);
         p.piece = static_cast<int32_t>(ceil_div(ceil_div(p.n_classes, p.pieces), 8) * 8);
         const int64_t blocks = p.n_rows * p.pieces;
-        if (blocks > INT32_MAX) return fail(MGG_ERR_UNSUPPORTED, "too many pieces for one launch");
+        if (!launchable(blocks, kPieceThreads)) return fail(MGG_ERR_UNSUPPORTED, "%s", refused);
         const dim3 grid(static_cast<unsigned>(blocks)), block(kPieceThreads);
         if (p.pieces == 1 && !p.grad) {
             hipLaunchKernelGGL((distill_stats_kernel<In, true>), grid, block, 0, stream, p);

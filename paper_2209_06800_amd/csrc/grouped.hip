@@ -945,8 +945,9 @@ mgg_status_t launched(const char *what)
     return e == hipSuccess ? MGG_OK : hip_fail(e, what);
 }
 
+// dry: nothing is launched, the answer is whether it could be
 template <typename T, bool B_ALONG, bool ODD>
-mgg_status_t rows_product(RowsArgs p, hipStream_t stream)
+mgg_status_t rows_product(RowsArgs p, bool dry, hipStream_t stream)
 {
     constexpr int N = Elem<T>::N;
     const int32_t cols = p.sink.n_cols;
@@ -958,12 +959,13 @@ mgg_status_t rows_product(RowsArgs p, hipStream_t stream)
         return most * p.col_tiles;
     };
     const char *const refused = "too many tiles for one launch";
-#define MGG_GRID(ROWS, COLS)                                                         \
-    const int64_t blocks = grid(ROWS, COLS);                                         \
-    if (blocks > INT32_MAX) return fail(MGG_ERR_UNSUPPORTED, "%s", refused);          \
+#define MGG_GRID(ROWS, COLS, THREADS)                                                      \
+    const int64_t blocks = grid(ROWS, COLS);                                               \
+    if (!launchable(blocks, THREADS)) return fail(MGG_ERR_UNSUPPORTED, "%s", refused);      \
+    if (dry) return MGG_OK;                                                                \
     const dim3 blocks_dim(static_cast<unsigned>(blocks))
     if (cols < N || p.depth < N) {
-        MGG_GRID(64, 64);
+        MGG_GRID(64, 64, 256);
         hipLaunchKernelGGL((tiny_rows_kernel<T, B_ALONG>), blocks_dim, dim3(256), 0, stream, p);
         return launched("grouped product launch");
     }
@@ -974,7 +976,7 @@ mgg_status_t rows_product(RowsArgs p, hipStream_t stream)
     if (p.n_rows <= 24 * static_cast<int64_t>(p.n_groups) || tiles <= kCus / 2) {
         // (8 wavefronts where blocks are few; 64 rows over 64 groups 1024 -> 2048 with 4: 40 us, with 8: 50; one row 4096 -> 4096 with
         // 8: 23 us, with 4: 27, as its 64 blocks fill a quarter of the chip)
-        MGG_GRID(32, 64);
+        MGG_GRID(32, 64, blocks < 2 * kCus ? 512 : 256);
         if (blocks < 2 * kCus) hipLaunchKernelGGL((grouped_few_rows_kernel<T, 64, 8, B_ALONG, ODD>), blocks_dim, dim3(512), 0, stream, p);
         else hipLaunchKernelGGL((grouped_few_rows_kernel<T, 64, 4, B_ALONG, ODD>), blocks_dim, dim3(256), 0, stream, p);
         return launched("grouped product launch");
@@ -982,20 +984,20 @@ mgg_status_t rows_product(RowsArgs p, hipStream_t stream)
     if constexpr (!ODD && sizeof(T) == 2) {
         // (a group's last piece is half full on average)
         if (large_pays((p.n_rows / 256 + present / 2) * ceil_div(cols, 256), (p.n_rows / 128 + present / 2) * ceil_div(cols, 128))) {
-            MGG_GRID(256, 256);
+            MGG_GRID(256, 256, 512);
             hipLaunchKernelGGL((grouped_rows_kernel<T, LARGE, B_ALONG, ODD>), blocks_dim, dim3(512), 0, stream, p);
             return launched("grouped product launch");
         }
     }
     if constexpr (sizeof(T) == 4) {
-        MGG_GRID(64, 64);
+        MGG_GRID(64, 64, 256);
         hipLaunchKernelGGL((grouped_rows_kernel<T, SMALL, B_ALONG, ODD>), blocks_dim, dim3(256), 0, stream, p);
         return launched("grouped product launch");
     } else if (cols <= 64) {
-        MGG_GRID(128, 64);
+        MGG_GRID(128, 64, 256);
         hipLaunchKernelGGL((grouped_rows_kernel<T, NARROW, B_ALONG, ODD>), blocks_dim, dim3(256), 0, stream, p);
     } else {
-        MGG_GRID(128, 128);
+        MGG_GRID(128, 128, 256);
         hipLaunchKernelGGL((grouped_rows_kernel<T, MEDIUM, B_ALONG, ODD>), blocks_dim, dim3(256), 0, stream, p);
     }
 #undef MGG_GRID
@@ -1003,19 +1005,22 @@ mgg_status_t rows_product(RowsArgs p, hipStream_t stream)
 }
 
 template <typename T>
-mgg_status_t rows_product_of(const RowsArgs &p, bool b_along, hipStream_t stream)
+mgg_status_t rows_product_of(const RowsArgs &p, bool b_along, bool dry, hipStream_t stream)
 {
     const bool odd = p.depth % Elem<T>::N != 0 || p.sink.n_cols % Elem<T>::N != 0;
-    if (b_along) return odd ? rows_product<T, true, true>(p, stream) : rows_product<T, true, false>(p, stream);
-    return odd ? rows_product<T, false, true>(p, stream) : rows_product<T, false, false>(p, stream);
+    if (b_along) return odd ? rows_product<T, true, true>(p, dry, stream) : rows_product<T, true, false>(p, dry, stream);
+    return odd ? rows_product<T, false, true>(p, dry, stream) : rows_product<T, false, false>(p, dry, stream);
 }
 
 template <typename T, bool ODD>
-mgg_status_t weight_product(WeightArgs p, const GradPlan &g, hipStream_t stream)
+mgg_status_t weight_product(WeightArgs p, const GradPlan &g, bool dry, hipStream_t stream)
 {
     p.row_tiles = static_cast<int32_t>(g.row_tiles);
     p.col_tiles = static_cast<int32_t>(g.col_tiles);
-    if (g.row_tiles > INT32_MAX || g.pieces * g.row_tiles > INT32_MAX / g.col_tiles) return fail(MGG_ERR_UNSUPPORTED, "too many tiles for one launch");
+    const int threads = !g.tiny && g.kind == LARGE ? 512 : 256;
+    if (g.row_tiles > INT32_MAX || g.pieces * g.row_tiles > INT32_MAX / g.col_tiles || !launchable(g.pieces * g.row_tiles * g.col_tiles, threads))
+        return fail(MGG_ERR_UNSUPPORTED, "too many tiles for one launch");
+    if (dry) return MGG_OK;
     const dim3 grid(static_cast<unsigned>(g.pieces * g.row_tiles * g.col_tiles));
     if (g.tiny) hipLaunchKernelGGL((tiny_weight_kernel<T>), grid, dim3(256), 0, stream, p);
     else if (g.kind == SMALL) hipLaunchKernelGGL((grouped_weight_kernel<T, SMALL, ODD>), grid, dim3(256), 0, stream, p);
@@ -1028,9 +1033,9 @@ mgg_status_t weight_product(WeightArgs p, const GradPlan &g, hipStream_t stream)
 }
 
 template <typename T>
-mgg_status_t weight_product_of(const WeightArgs &p, const GradPlan &g, hipStream_t stream)
+mgg_status_t weight_product_of(const WeightArgs &p, const GradPlan &g, bool dry, hipStream_t stream)
 {
-    return p.d_in % Elem<T>::N != 0 || p.d_out % Elem<T>::N != 0 ? weight_product<T, true>(p, g, stream) : weight_product<T, false>(p, g, stream);
+    return p.d_in % Elem<T>::N != 0 || p.d_out % Elem<T>::N != 0 ? weight_product<T, true>(p, g, dry, stream) : weight_product<T, false>(p, g, dry, stream);
 }
 
 mgg_status_t join_pieces(const JoinArgs &p, hipStream_t stream)
@@ -1047,7 +1052,6 @@ mgg_status_t mask_rows(MaskArgs m, int64_t pieces, hipStream_t stream)
     const int64_t vecs = m.d_out < V ? m.d_out : ceil_div(m.d_out, V);
     m.lanes_log2 = ceil_log2(vecs) < 6 ? ceil_log2(vecs) : 6;
     const dim3 grid(static_cast<unsigned>(pieces), static_cast<unsigned>(ceil_div(vecs, static_cast<int64_t>(1) << m.lanes_log2)));
-    if (grid.y > 65535) return fail(MGG_ERR_UNSUPPORTED, "too many columns for one launch");
     if (m.d_out < V) hipLaunchKernelGGL((mask_rows_kernel<T, 1>), grid, dim3(256), 0, stream, m);
     else hipLaunchKernelGGL((mask_rows_kernel<T, V>), grid, dim3(256), 0, stream, m);
     return launched("mask launch");
@@ -1063,7 +1067,7 @@ mgg_status_t launch_update_grouped(int64_t n_rows, int32_t n_groups, const int64
     p.a = a; p.w = w; p.ptr = group_ptr; p.n_rows = n_rows; p.ld_a = ld_a; p.n_groups = n_groups;
     p.w_group = static_cast<int64_t>(d_in) * d_out; p.ld_w = d_out; p.depth = d_in;
     p.sink = Sink{out, ld_out, bias, d_out, out_dtype == MGG_BF16, relu, 0};
-    return dtype == MGG_BF16 ? rows_product_of<Bf16>(p, false, stream) : rows_product_of<float>(p, false, stream);
+    return dtype == MGG_BF16 ? rows_product_of<Bf16>(p, false, false, stream) : rows_product_of<float>(p, false, false, stream);
 }
 
 size_t grouped_grad_workspace(int64_t n_rows, int32_t n_groups, int32_t d_in, int32_t d_out, mgg_dtype_t dtype, bool relu)
@@ -1079,6 +1083,24 @@ mgg_status_t launch_update_grouped_grad(const GroupedGrad &q, void *workspace, h
     const void *dz = q.grad_out;
     int64_t ld_dz = q.ld_grad;
     mgg_status_t s = MGG_OK;
+    auto rows = [&](bool dry) {
+        RowsArgs p{};
+        p.a = dz; p.w = q.w; p.ptr = q.group_ptr; p.n_rows = q.n_rows; p.ld_a = ld_dz; p.n_groups = q.n_groups;
+        p.w_group = static_cast<int64_t>(q.d_in) * q.d_out; p.ld_w = q.d_out; p.depth = q.d_out;
+        p.sink = Sink{q.grad_a, q.ld_grad_a, nullptr, q.d_in, q.grad_a_dtype == MGG_BF16, 0, 0};
+        return bf16 ? rows_product_of<Bf16>(p, true, dry, stream) : rows_product_of<float>(p, true, dry, stream);
+    };
+    auto weights = [&](bool dry) {
+        WeightArgs p{};
+        p.a = q.a; p.dz = dz; p.ptr = q.group_ptr; p.n_rows = q.n_rows; p.ld_a = q.ld_a; p.ld_dz = ld_dz;
+        p.n_groups = q.n_groups; p.d_in = q.d_in; p.d_out = q.d_out; p.step = g.step;
+        p.sink = Sink{q.grad_w, q.d_out, nullptr, q.d_out, q.grad_w_dtype == MGG_BF16, 0, q.add_w};
+        p.part = reinterpret_cast<float *>(ws + g.part);
+        return bf16 ? weight_product_of<Bf16>(p, g, dry, stream) : weight_product_of<float>(p, g, dry, stream);
+    };
+    // what does not fit a launch is refused before anything is written
+    if (q.grad_a && (s = rows(true)) != MGG_OK) return s;
+    if (q.grad_w && (s = weights(true)) != MGG_OK) return s;
     if (q.n_rows > 0 && (q.grad_bias || (q.relu && (q.grad_a || q.grad_w)))) {
         MaskArgs m{};
         m.grad = q.grad_out; m.ptr = q.group_ptr; m.n_rows = q.n_rows; m.ld_grad = q.ld_grad; m.n_groups = q.n_groups; m.d_out = q.d_out; m.step = g.mask_step;
@@ -1096,20 +1118,11 @@ mgg_status_t launch_update_grouped_grad(const GroupedGrad &q, void *workspace, h
         if (s != MGG_OK) return s;
     }
     if (q.grad_a) {
-        RowsArgs p{};
-        p.a = dz; p.w = q.w; p.ptr = q.group_ptr; p.n_rows = q.n_rows; p.ld_a = ld_dz; p.n_groups = q.n_groups;
-        p.w_group = static_cast<int64_t>(q.d_in) * q.d_out; p.ld_w = q.d_out; p.depth = q.d_out;
-        p.sink = Sink{q.grad_a, q.ld_grad_a, nullptr, q.d_in, q.grad_a_dtype == MGG_BF16, 0, 0};
-        s = bf16 ? rows_product_of<Bf16>(p, true, stream) : rows_product_of<float>(p, true, stream);
+        s = rows(false);
         if (s != MGG_OK) return s;
     }
     if (q.grad_w) {
-        WeightArgs p{};
-        p.a = q.a; p.dz = dz; p.ptr = q.group_ptr; p.n_rows = q.n_rows; p.ld_a = q.ld_a; p.ld_dz = ld_dz;
-        p.n_groups = q.n_groups; p.d_in = q.d_in; p.d_out = q.d_out; p.step = g.step;
-        p.sink = Sink{q.grad_w, q.d_out, nullptr, q.d_out, q.grad_w_dtype == MGG_BF16, 0, q.add_w};
-        p.part = reinterpret_cast<float *>(ws + g.part);
-        s = bf16 ? weight_product_of<Bf16>(p, g, stream) : weight_product_of<float>(p, g, stream);
+        s = weights(false);
         if (s != MGG_OK || !g.step) return s;
         s = join_pieces(JoinArgs{reinterpret_cast<float *>(ws + g.part), q.group_ptr, q.grad_w, q.n_rows, static_cast<int64_t>(q.d_in) * q.d_out, q.n_groups, g.step,
                                  static_cast<int32_t>(g.pieces), q.grad_w_dtype == MGG_BF16, q.add_w, 1}, stream);

@@ -63,7 +63,7 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(const EmbedArgs<In, Out
 }
 
 template <typename In, typename Out, typename Id>
-hipError_t embed_typed(int64_t n, const void *ids, int64_t table_rows, const void *table, int32_t dim, int64_t ld_table, float scale, void *out, int64_t ld_out,
+mgg_status_t embed_typed(int64_t n, const void *ids, int64_t table_rows, const void *table, int32_t dim, int64_t ld_table, float scale, void *out, int64_t ld_out,
                        hipStream_t stream)
 {
     constexpr int VEC = sizeof(In) == 4 && sizeof(Out) == 4 ? 4 : 8;
@@ -74,16 +74,19 @@ hipError_t embed_typed(int64_t n, const void *ids, int64_t table_rows, const voi
                                    lanes_log2, scale};
     const int64_t slabs = ceil_div(vecs, static_cast<int64_t>(1) << lanes_log2);
     const int64_t rows_per_block = kThreads >> lanes_log2;
-    const bool four = n / rows_per_block >= 4096;           // blocks enough for the chip at four rows per thread
-    const dim3 grid(static_cast<unsigned>(ceil_div(n, rows_per_block * (four ? 4 : 1))), static_cast<unsigned>(slabs < 1024 ? slabs : 1024));
+    const bool four = dim >= VEC && n / rows_per_block >= 4096;         // blocks enough for the chip at four rows per thread
+    const int64_t blocks = ceil_div(n, rows_per_block * (four ? 4 : 1));
+    if (!launchable(blocks, kThreads)) return fail(MGG_ERR_UNSUPPORTED, "%lld ids of %d columns need too many threads for one launch", (long long)n, dim);
+    const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(slabs < 1024 ? slabs : 1024));
     if (dim < VEC) {
-        hipLaunchKernelGGL((embed_kernel<In, Out, Id, 1, 1>), dim3(static_cast<unsigned>(ceil_div(n, rows_per_block)), grid.y), dim3(kThreads), 0, stream, p);
+        hipLaunchKernelGGL((embed_kernel<In, Out, Id, 1, 1>), grid, dim3(kThreads), 0, stream, p);
     } else if (four) {
         hipLaunchKernelGGL((embed_kernel<In, Out, Id, VEC, 4>), grid, dim3(kThreads), 0, stream, p);
     } else {
         hipLaunchKernelGGL((embed_kernel<In, Out, Id, VEC, 1>), grid, dim3(kThreads), 0, stream, p);
     }
-    return hipGetLastError();
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? MGG_OK : hip_fail(e, "lookup kernel launch");
 }
 
 // ---- the ids in order ----------------------------------------------------------------------------------------
@@ -586,8 +589,9 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(const SumArgs<In, 
     put_row<In, Out, VEC>(p, id, c, c + VEC <= p.dim ? c : p.dim - VEC, sum);
 }
 
+// the sort and the sums; what does not fit a launch is refused before either
 template <typename In, typename Out, int VEC>
-hipError_t embed_sum(const EmbedGradPlan &s, SumArgs<In, Out> p, hipStream_t stream)
+mgg_status_t embed_sum(const EmbedGradPlan &s, SumArgs<In, Out> p, mgg_index_t id_type, const void *ids, char *ws, hipStream_t stream)
 {
     const int64_t vecs = ceil_div(p.dim, VEC);
     p.lanes_log2 = ceil_log2(vecs) < 6 ? ceil_log2(vecs) : 6;
@@ -597,11 +601,18 @@ hipError_t embed_sum(const EmbedGradPlan &s, SumArgs<In, Out> p, hipStream_t str
     const int64_t fill = 32768 / (static_cast<int64_t>(p.dim) * static_cast<int64_t>(sizeof(Out)));
     p.fill_rows = static_cast<int32_t>(fill < 1 ? 1 : (fill < kWave ? fill : kWave));
     const int64_t fill_blocks = p.accumulate ? 0 : ceil_div(p.table_rows, static_cast<int64_t>(p.fill_rows) * (kThreads / kWave));
-    if (p.sum_blocks + fill_blocks > INT32_MAX || s.chunks * p.slabs > INT32_MAX) return hipErrorInvalidConfiguration;
-    if (p.sum_blocks + fill_blocks == 0) return hipSuccess;
+    if (!launchable(p.sum_blocks + fill_blocks, kThreads) || !launchable(s.chunks * p.slabs, kThreads))
+        return fail(MGG_ERR_UNSUPPORTED, "%lld ids of %d columns need too many threads for one launch", (long long)p.n, p.dim);
+    if (p.sum_blocks + fill_blocks == 0) return MGG_OK;
+    if (p.n > 0) {
+        const hipError_t e = id_type == MGG_I64 ? sort_ids<int64_t>(s, p.n, ids, p.table_rows, ws, &p.keys, &p.pos, stream)
+                                                : sort_ids<int32_t>(s, p.n, ids, p.table_rows, ws, &p.keys, &p.pos, stream);
+        if (e != hipSuccess) return hip_fail(e, "sort kernel launch");
+    }
     hipLaunchKernelGGL((embed_sum_kernel<In, Out, VEC>), dim3(static_cast<unsigned>(p.sum_blocks + fill_blocks)), dim3(kThreads), 0, stream, p);
     if (s.chunks > 1) hipLaunchKernelGGL((embed_join_kernel<In, Out, VEC>), dim3(static_cast<unsigned>(s.chunks * p.slabs)), dim3(kThreads), 0, stream, p);
-    return hipGetLastError();
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? MGG_OK : hip_fail(e, "table gradient kernel launch");
 }
 
 }  // namespace
@@ -610,14 +621,12 @@ mgg_status_t launch_embed(int64_t n, mgg_index_t id_type, const void *ids, int64
                           int64_t ld_table, float scale, mgg_dtype_t out_dtype, void *out, int64_t ld_out, hipStream_t stream)
 {
     if (n > static_cast<int64_t>(INT32_MAX)) return fail(MGG_ERR_UNSUPPORTED, "%lld ids", (long long)n);
-    hipError_t e;
 #define MGG_EMBED(IN, OUT)                                                                                                              \
-    e = id_type == MGG_I64 ? embed_typed<IN, OUT, int64_t>(n, ids, table_rows, table, dim, ld_table, scale, out, ld_out, stream)         \
-                           : embed_typed<IN, OUT, int32_t>(n, ids, table_rows, table, dim, ld_table, scale, out, ld_out, stream)
+    return id_type == MGG_I64 ? embed_typed<IN, OUT, int64_t>(n, ids, table_rows, table, dim, ld_table, scale, out, ld_out, stream)         \
+                                : embed_typed<IN, OUT, int32_t>(n, ids, table_rows, table, dim, ld_table, scale, out, ld_out, stream)
     if (table_dtype == MGG_BF16) { if (out_dtype == MGG_BF16) MGG_EMBED(Bf16, Bf16); else MGG_EMBED(Bf16, float); }
     else { if (out_dtype == MGG_BF16) MGG_EMBED(float, Bf16); else MGG_EMBED(float, float); }
 #undef MGG_EMBED
-    return e == hipSuccess ? MGG_OK : hip_fail(e, "lookup kernel launch");
 }
 
 size_t embed_grad_workspace(int64_t n, int64_t table_rows, int32_t dim) { return plan_embed_grad(n, table_rows, dim).bytes; }
@@ -628,23 +637,16 @@ mgg_status_t launch_embed_grad(int64_t n, mgg_index_t id_type, const void *ids, 
 {
     const EmbedGradPlan s = plan_embed_grad(n, table_rows, dim);
     char *ws = static_cast<char *>(workspace);
-    const uint32_t *keys = nullptr, *pos = nullptr;
-    hipError_t e = hipSuccess;
-    if (n > 0) {
-        e = id_type == MGG_I64 ? sort_ids<int64_t>(s, n, ids, table_rows, ws, &keys, &pos, stream) : sort_ids<int32_t>(s, n, ids, table_rows, ws, &keys, &pos, stream);
-        if (e != hipSuccess) return hip_fail(e, "sort kernel launch");
-    }
 #define MGG_SUM(IN, OUT)                                                                                                                                      \
     do {                                                                                                                                                      \
-        const SumArgs<IN, OUT> p{keys, pos, static_cast<const IN *>(grad), static_cast<OUT *>(out), reinterpret_cast<float *>(ws + s.part), n, table_rows,       \
+        const SumArgs<IN, OUT> p{nullptr, nullptr, static_cast<const IN *>(grad), static_cast<OUT *>(out), reinterpret_cast<float *>(ws + s.part), n, table_rows,       \
                                  ld_grad, ld_out, s.ld_part, 0, dim, s.chunk, static_cast<int32_t>(s.chunks), 0, 0, 0, scale, accumulate};                         \
         constexpr int VEC = 16 / sizeof(IN);                                                                                                                  \
-        e = dim < 8 ? embed_sum<IN, OUT, 1>(s, p, stream) : embed_sum<IN, OUT, VEC>(s, p, stream);                                                              \
+        return dim < 8 ? embed_sum<IN, OUT, 1>(s, p, id_type, ids, ws, stream) : embed_sum<IN, OUT, VEC>(s, p, id_type, ids, ws, stream);                      \
     } while (0)
     if (grad_dtype == MGG_BF16) { if (out_dtype == MGG_BF16) MGG_SUM(Bf16, Bf16); else MGG_SUM(Bf16, float); }
     else { if (out_dtype == MGG_BF16) MGG_SUM(float, Bf16); else MGG_SUM(float, float); }
 #undef MGG_SUM
-    return e == hipSuccess ? MGG_OK : hip_fail(e, "table gradient kernel launch");
 }
 
 }  // namespace mgg

@@ -70,6 +70,8 @@ inline int ceil_log2(int64_t v)
     return b;
 }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// a launch has fewer than 2^31 blocks and 2^32 threads along its first axis
+inline bool launchable(int64_t blocks, int threads) { return blocks <= INT32_MAX && blocks * threads <= static_cast<int64_t>(UINT32_MAX); }
 inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 }  // namespace train

@@ -703,3 +703,25 @@ def test_calls_on_another_stream():
     assert all(bool(torch.isnan(t).all()) for t in scribble)
     assert all(torch.equal(a, b) for a, b in zip(got, wants))
     assert len(want) == 5
+
+
+# a launch has fewer than 2^32 threads; what would need more is refused before anything is launched
+LARGE_WS = dict(bytes=2 ** 62)
+TOO_LARGE = [
+    (embed_call, dict(n=2 ** 31 - 1, dim=2, ld=2, ldo=2, tt=1, ot=1)),
+    (embed_grad_call, dict(n=2 ** 30, dim=1, ld=1, ldo=1, gt=1, **LARGE_WS)),
+    (grouped_call, dict(n=2 ** 31 - 1, g=1, k=1, m=1, lda=1, ldo=1)),
+    (grouped_call, dict(n=2 ** 31 - 1, g=1)),
+    (grouped_call, dict(n=2 ** 31 - 1, g=1, m=128, ldo=128, at=1, wt=1, ot=1)),
+    (grouped_grad_call, dict(n=2 ** 31 - 1, g=1, act=1, out=P, ldo=8, db=P, **LARGE_WS)),
+    (grouped_grad_call, dict(g=65535, k=2 ** 22, m=1, ldg=1, lda=2 ** 22, da=None, db=P, **LARGE_WS)),
+    (distill_call, dict(n=2 ** 31 - 2, **LARGE_WS)),
+    (distill_call, dict(n=2 ** 25, c=4096, ldz=4096, ldg=4096, **LARGE_WS)),
+    (distill_call, dict(n=2 ** 25, c=4096, ldz=4096, grad=None, ldg=0, **LARGE_WS)),
+]
+
+
+@pytest.mark.parametrize("call,change", TOO_LARGE, ids=lambda v: str(v) if isinstance(v, dict) else None)
+def test_more_threads_than_a_launch_has_are_refused(call, change):
+    assert call(**change) == UNSUPPORTED
+    assert len(binding.lib().mgg_last_error()) > 0
