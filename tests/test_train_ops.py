@@ -725,3 +725,78 @@ TOO_LARGE = [
 def test_more_threads_than_a_launch_has_are_refused(call, change):
     assert call(**change) == UNSUPPORTED
     assert len(binding.lib().mgg_last_error()) > 0
+
+
+def _some_calls(seed):
+    """One call of every operator on inputs of its own; returns a function that makes the calls and gives their outputs."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    n, rows, dim, groups, d_out, classes, k = 12000, 701, 264, 6, 136, 1001, 9
+    ids = torch.randint(-1, rows, (n,), device="cuda", generator=g)
+    ids[::3] = seed % rows                                   # a common one, whose sum reaches over many chunks
+    rnd = lambda *shape: torch.randn(*shape, device="cuda", generator=g)
+    table, w, bias, up = rnd(rows, dim).bfloat16(), rnd(groups, dim, d_out).bfloat16(), rnd(groups, d_out), rnd(n, d_out).bfloat16()
+    ptr = torch.tensor([0, 5, 5, 3000, 9000, 11000, n], device="cuda")
+    logits, top, top_ids = rnd(n, classes), rnd(n, k), torch.randint(-1, classes, (n, k), device="cuda", generator=g)
+
+    def call(stream=None):
+        a = binding.mgg_embed(ids, table, scale=1.5, stream=stream)
+        out = binding.mgg_update_grouped(ptr, a, w, bias, "relu", stream=stream)
+        grads = binding.mgg_update_grouped_grad(ptr, up, a, w, "relu", out=out, need_bias=True, stream=stream)
+        back = binding.mgg_embed_grad(ids, grads[0], rows, scale=1.5, stream=stream)
+        loss, grad = binding.mgg_distill_loss(logits, top_ids, top, temperature=2.0, need_grad=True, stream=stream)
+        return (a, out, *grads, back, loss, grad)
+
+    return call
+
+
+@pytest.mark.gpu
+def test_the_same_call_gives_the_same_bits():
+    call = _some_calls(1)
+    first = call()
+    for _ in range(3):
+        for x, y in zip(first, call()):
+            assert torch.equal(x, y)
+
+
+@pytest.mark.gpu
+def test_two_streams_at_once():
+    calls, streams = [_some_calls(s) for s in (2, 3)], [torch.cuda.Stream() for _ in range(2)]
+    alone = [c() for c in calls]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        both = [c(stream=s) for _ in range(2) for c, s in zip(calls, streams)]
+        torch.cuda.synchronize()
+        for i, got in enumerate(both):
+            for x, y in zip(alone[i % 2], got):
+                assert torch.equal(x, y)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("counts,d_in,d_out", [((3, 0, 40, 1), 20, 12), ((700, 9, 300), 130, 65), ((5, 6), 2, 3)])
+def test_linear_gradients_against_differences(counts, d_in, d_out):
+    """Products and lookups are linear in their weights, so a central difference of any step is exact but for rounding: an output of d terms is
+    off by (d + 2) 2^-24 of the sum of their magnitudes, and so is a gradient of as many.  Inputs lie on a grid of 2^-6, so that the
+    steps are exact."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    grid = lambda *shape: (torch.randn(*shape, device="cuda", generator=g).clamp(-3, 3) * 64).round() / 64
+    n, groups = sum(counts), len(counts)
+    ptr = torch.tensor([0, *np.cumsum(counts)], device="cuda")
+    a, w, up = grid(n, d_in), grid(groups, d_in, d_out), grid(n, d_out)
+    grad_a, grad_w = binding.mgg_update_grouped_grad(ptr, up, a, w)
+    eps = 2.0 ** -24
+    absolute = lambda x, y: binding.mgg_update_grouped(ptr, x.abs(), y.abs()).double() * 1.001       # (fp32 itself, hence the 1.001)
+    for x, grad, terms, step in ((a, grad_a, d_out, grid(n, d_in)), (w, grad_w, max(counts), grid(groups, d_in, d_out))):
+        plus, minus = ((x + step, w), (x - step, w)) if x is a else ((a, x + step), (a, x - step))
+        difference = (binding.mgg_update_grouped(ptr, *plus).double() - binding.mgg_update_grouped(ptr, *minus).double()) * up.double() / 2
+        off = (d_in + 2) * eps * ((absolute(*plus) + absolute(*minus)) * up.double().abs()).sum() / 2
+        size_a, size_w = binding.mgg_update_grouped_grad(ptr, up.abs(), a.abs(), w.abs())
+        off += (terms + 2) * eps * ((size_a if x is a else size_w).double() * step.double().abs()).sum() * 1.001
+        # (sums in 64 bits round by 2^-53 a term, some 2^-33 of what the above allows for)
+        assert abs(float((grad.double() * step.double()).sum() - difference.sum())) <= float(off)
+    rows = 37
+    ids = torch.randint(-1, rows, (n,), device="cuda", generator=g)
+    table, step, up = grid(rows, d_in), grid(rows, d_in), grid(n, d_in)
+    difference = (binding.mgg_embed(ids, table + step).double() - binding.mgg_embed(ids, table - step).double()) * up.double() / 2
+    grad = binding.mgg_embed_grad(ids, up, rows).double()
+    off = (n + 2) * eps * (binding.mgg_embed_grad(ids, up.abs(), rows).double() * step.double().abs()).sum() * 1.001
+    assert abs(float((grad * step.double()).sum() - difference.sum())) <= float(off)
