@@ -459,7 +459,7 @@ __device__ __forceinline__ uint64_t ids_present(const uint32_t *keys, int64_t n,
 
 // columns [c, c + VEC) of a finished row; with the last vector moved back to `col` the columns before c are the neighbour's
 template <typename In, typename Out, int VEC>
-__device__ __forceinline__ void put_row(const SumArgs<In, Out> &p, uint32_t row, int c, int col, const float (&sum)[VEC])
+__device__ __forceinline__ void put_row(const SumArgs<In, Out> &p, uint32_t row, int64_t c, int64_t col, const float (&sum)[VEC])
 {
     Out *o = p.out + static_cast<int64_t>(row) * p.ld_out;
     float v[VEC];
@@ -495,16 +495,16 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(const SumArgs<In, O
         const float zero[VO] = {};
         for (int r = lane >> p.lanes_log2; r < count; r += kWave >> p.lanes_log2)
             if ((rows >> r) & 1)
-                for (int c = (lane & (lanes - 1)) * VO; c < p.dim; c += lanes * VO)
+                for (int64_t c = (lane & (lanes - 1)) * VO; c < p.dim; c += lanes * VO)
                     store_n<VO>(p.out + (row0 + r) * p.ld_out + (c + VO <= p.dim ? c : p.dim - VO), zero);
         return;
     }
     constexpr int U = 8;
     const int64_t group = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) >> p.lanes_log2;
     const int64_t chunk = group / p.slabs;
-    const int c = static_cast<int>(((group % p.slabs) << p.lanes_log2) + (threadIdx.x & (lanes - 1))) * VEC;
+    const int64_t c = (((group % p.slabs) << p.lanes_log2) + (threadIdx.x & (lanes - 1))) * VEC;
     if (chunk >= p.chunks || c >= p.dim) return;
-    const int col = c + VEC <= p.dim ? c : p.dim - VEC;
+    const int64_t col = c + VEC <= p.dim ? c : p.dim - VEC;
     const int64_t beg = chunk * p.chunk, end = beg + p.chunk < p.n ? beg + p.chunk : p.n;
     const uint32_t none = static_cast<uint32_t>(p.table_rows);
     uint32_t cur = p.keys[beg];
@@ -564,7 +564,7 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(const SumArgs<In, 
     if (p.keys[beg] == id && beg > 0 && p.keys[beg - 1] == id) return;              // it began in an earlier one
     const int64_t last = (wave_lower_bound(p.keys, end, p.n, id + 1, threadIdx.x & 63) - 1) / p.chunk;
     const int lanes = 1 << p.lanes_log2, groups = kThreads >> p.lanes_log2, group = threadIdx.x >> p.lanes_log2;
-    const int c = static_cast<int>(((blockIdx.x % p.slabs) << p.lanes_log2) + (threadIdx.x & (lanes - 1))) * VEC;
+    const int64_t c = (static_cast<int64_t>((blockIdx.x % p.slabs) << p.lanes_log2) + (threadIdx.x & (lanes - 1))) * VEC;
     const int64_t count = last - chunk + 1, share = (count + groups - 1) / groups, from = group * share, to = from + share < count ? from + share : count;
     float sum[VEC];
 #pragma unroll

@@ -800,3 +800,34 @@ def test_linear_gradients_against_differences(counts, d_in, d_out):
     grad = binding.mgg_embed_grad(ids, up, rows).double()
     off = (n + 2) * eps * (binding.mgg_embed_grad(ids, up.abs(), rows).double() * step.double().abs()).sum() * 1.001
     assert abs(float((grad * step.double()).sum() - difference.sum())) <= float(off)
+
+
+@gpu
+def test_rows_as_long_as_32_bits_count():
+    """2^31 - 1 columns: the last vectors' columns, and what a loop's step adds to them, lie past 32 bits.  Values stand at both ends and in the
+    middle, zeros elsewhere; the elements around the matrices stay as they were."""
+    dim, rows, guard = 2 ** 31 - 1, 3, 4096
+    marks = torch.tensor([0, 1, 511, 2 ** 30, 2 ** 30 + 1, *range(dim - 20, dim)], device=DEV)
+
+    def guarded(n):
+        buf = torch.full((2 * guard + n * dim,), 9.0, dtype=BF16, device=DEV)
+        return buf, buf[guard: guard + n * dim].view(n, dim)
+
+    def untouched(buf):
+        return bool((buf[:guard] == 9).all()) and bool((buf[-guard:] == 9).all())
+
+    values = (torch.arange(marks.numel(), device=DEV) + 1).to(BF16)
+    grad = torch.zeros(3, dim, dtype=BF16, device=DEV)
+    for i in range(3):
+        grad[i, marks] = values * (i + 1)
+    buf, out = guarded(rows)
+    ids = torch.tensor([0, 2, 0], device=DEV)
+    binding.mgg_embed_grad(ids, grad, rows, out=out)
+    assert untouched(buf)
+    for v, factor in enumerate((4, 0, 2)):
+        assert torch.equal(out[v, marks], (values.float() * factor).to(BF16))
+        assert int((out[v] != 0).sum()) == (marks.numel() if factor else 0)
+    del buf, out
+    buf, out = guarded(2)
+    binding.mgg_embed(torch.tensor([2, -1], device=DEV), grad, out=out)
+    assert untouched(buf) and torch.equal(out[0], grad[2]) and not bool((out[1] != 0).any())
