@@ -5,6 +5,7 @@ Tolerances count roundings: a sum of K fp32 products or terms is off by at most 
 order (2^-24 each where every addition rounds to nearest; the matrix instruction is given the factor 2), and an output by half a
 step of its type, finfo(t).eps / 2 of the value.
 """
+import ctypes
 import itertools
 
 import numpy as np
@@ -831,3 +832,46 @@ def test_rows_as_long_as_32_bits_count():
     buf, out = guarded(2)
     binding.mgg_embed(torch.tensor([2, -1], device=DEV), grad, out=out)
     assert untouched(buf) and torch.equal(out[0], grad[2]) and not bool((out[1] != 0).any())
+
+
+class _KernelNode(ctypes.Structure):            # hipKernelNodeParams
+    _fields_ = [("block", ctypes.c_uint * 3), ("extra", ctypes.c_void_p), ("func", ctypes.c_void_p), ("grid", ctypes.c_uint * 3),
+                ("params", ctypes.c_void_p), ("shared", ctypes.c_uint)]
+
+
+def launches(call):
+    """(blocks along the first axis, threads of a block) of every kernel that the call launches, from a graph that it is captured into."""
+    with open("/proc/self/maps") as f:
+        path = next(line.split()[-1] for line in f if "libamdhip64" in line)        # the runtime that torch has loaded
+    hip = ctypes.CDLL(path)
+    graph = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(graph):
+        kept = call()
+    raw, count = ctypes.c_void_p(graph.raw_cuda_graph()), ctypes.c_size_t(0)
+    assert hip.hipGraphGetNodes(raw, None, ctypes.byref(count)) == 0
+    nodes = (ctypes.c_void_p * count.value)()
+    assert hip.hipGraphGetNodes(raw, nodes, ctypes.byref(count)) == 0
+    shapes = []
+    for node in nodes:
+        kind, p = ctypes.c_int(-1), _KernelNode()
+        assert hip.hipGraphNodeGetType(ctypes.c_void_p(node), ctypes.byref(kind)) == 0 and kind.value == 0          # a kernel
+        assert hip.hipGraphKernelNodeGetParams(ctypes.c_void_p(node), ctypes.byref(p)) == 0
+        shapes.append((p.grid[0], p.block[0]))
+    del kept
+    return shapes
+
+
+@gpu
+@pytest.mark.parametrize("n,tile", [(25, 128), (37, 128), (100, 128), (128, 128), (129, 128), (255, 128), (256, 128), (300, 256), (512, 256)])
+def test_one_group_of_few_rows_and_many_columns(n, tile):
+    """A head of 32,000 columns.  Pieces of one group are known: 25 to 256 rows are one piece of 256 or two of 128, and 125 large tiles leave
+    more of the chip idle than 250 or 500 medium ones.  (Blocks of 512 threads take large tiles, those of 256 medium ones.)"""
+    d_in, d_out = 72, 32000
+    g = torch.Generator().manual_seed(n)
+    a, w = torch.randn(n, d_in, generator=g).bfloat16(), (torch.randn(1, d_in, d_out, generator=g) * d_in ** -0.5).bfloat16()
+    ptr = torch.tensor([0, n])
+    args = (ptr.to(DEV), a.to(DEV), w.to(DEV))
+    ref, mag = grouped_reference(ptr, a, w, None, "none")
+    assert_within(binding.mgg_update_grouped(*args), ref, (d_in + 2) * U * mag + half_step(BF16) * ref.abs())
+    out = torch.empty(n, d_out, dtype=BF16, device=DEV)
+    assert launches(lambda: binding.mgg_update_grouped(*args, out=out)) == [((n // tile + 1) * (d_out // tile), 2 * tile)]
