@@ -59,38 +59,45 @@ __device__ __forceinline__ int wave_scan(int v)
 
 __device__ __forceinline__ int pieces_in(int32_t rows, int step) { return rows / step + (rows % step != 0); }
 
-// pieces of `step` rows in the first n_groups groups, by a wavefront, a group per lane; `most` where overlapping groups would give more
-__device__ __forceinline__ int count_pieces(const int64_t *ptr, int n_groups, int64_t n_rows, int step, int most)
+// pieces of `step` rows in the first n_groups groups, those of groups of fewer than `least` left out, by a wavefront, a group per lane;
+// `most` where overlapping groups would give more
+__device__ __forceinline__ int count_pieces(const int64_t *ptr, int n_groups, int64_t n_rows, int step, int most, int least = 1)
 {
     int total = 0;
     for (int g0 = 0; g0 < n_groups; g0 += kWave) {
         int32_t lo, hi;
         group_range(ptr, g0 + (threadIdx.x & 63), n_groups, n_rows, &lo, &hi);
-        total = min(total + min(__builtin_amdgcn_readlane(wave_scan(pieces_in(hi - lo, step)), 63), most), most);
+        const int pieces = pieces_in(hi - lo, step);
+        total = min(total + min(__builtin_amdgcn_readlane(wave_scan(pieces < least ? 0 : pieces), 63), most), most);
     }
     return total;
 }
 
-// piece number `index`, found by every wavefront for itself, 64 groups at a time
-__device__ __forceinline__ bool find_piece(const int64_t *ptr, int n_groups, int64_t n_rows, int step, int index, Span *s)
+// piece number `index`, found by every wavefront for itself, 64 groups at a time; SLOT: also its number among the pieces of groups of
+// several
+template <bool SLOT = false>
+__device__ __forceinline__ bool find_piece(const int64_t *ptr, int n_groups, int64_t n_rows, int step, int index, Span *s, int *slot = nullptr)
 {
-    int before = 0;
+    int before = 0, slots = 0;
     for (int g0 = 0; g0 < n_groups; g0 += kWave) {
         int32_t lo, hi;
         group_range(ptr, g0 + (threadIdx.x & 63), n_groups, n_rows, &lo, &hi);
         const int count = pieces_in(hi - lo, step), incl = wave_scan(count);
+        const int several = count < 2 ? 0 : count, several_incl = SLOT ? wave_scan(several) : 0;
         const uint64_t past = __ballot(before + incl > index);
         if (past) {
             const int at = __builtin_amdgcn_readfirstlane(__ffsll(static_cast<unsigned long long>(past)) - 1);
-            const int first = __builtin_amdgcn_readlane(lo, at) + (index - before - __builtin_amdgcn_readlane(incl - count, at)) * step;
+            const int in = index - before - __builtin_amdgcn_readlane(incl - count, at), first = __builtin_amdgcn_readlane(lo, at) + in * step;
             const int last = __builtin_amdgcn_readlane(hi, at);
             if (first < __builtin_amdgcn_readlane(lo, at) || first >= last) return false;       // (sums of overlapping groups can overflow)
             s->group = g0 + at;
             s->row = first;
             s->end = last - first < step ? last : first + step;
+            if constexpr (SLOT) *slot = slots + __builtin_amdgcn_readlane(several_incl - several, at) + in;
             return true;
         }
         before += __builtin_amdgcn_readlane(incl, 63);
+        if constexpr (SLOT) slots += __builtin_amdgcn_readlane(several_incl, 63);
     }
     return false;
 }
@@ -643,23 +650,27 @@ struct WeightArgs {
     int64_t n_rows, ld_a, ld_dz;
     int32_t n_groups, d_in, d_out, row_tiles, col_tiles;
     int32_t step;           // rows of a piece; 0: a group is one
+    int32_t slots;          // partial sums there is room for: one for each piece of the groups of several
     Sink sink;              // of group 0
-    float *part;            // of piece 0
+    float *part;            // the first partial sums
 };
 
 // The rows of group or piece number `index`, and where its product goes: to the result where it is all of a group, else to the partial sums
+template <bool PIECES>
 __device__ __forceinline__ bool weight_span(const WeightArgs &p, int index, Span *s, Sink *sink)
 {
     int64_t at;
     *sink = p.sink;
-    if (p.step) {
-        if (!find_piece(p.ptr, p.n_groups, p.n_rows, p.step, index, s)) return false;
+    if (PIECES && p.step) {
+        int slot;
+        if (!find_piece<true>(p.ptr, p.n_groups, p.n_rows, p.step, index, s, &slot)) return false;
         int32_t lo, hi;
         group_range(p.ptr, s->group, p.n_groups, p.n_rows, &lo, &hi);
         at = s->group;
         if (hi - lo > p.step) {
+            if (slot >= p.slots) return false;      // (overlapping groups)
             *sink = Sink{p.part, p.sink.ld, nullptr, p.sink.n_cols, 0, 0, 0};
-            at = index;
+            at = slot;
         }
     } else {
         s->group = index;
@@ -670,7 +681,7 @@ __device__ __forceinline__ bool weight_span(const WeightArgs &p, int index, Span
     return true;
 }
 
-// weights' gradient: tiles of [d_in x d_out] per group, or per piece of `step` rows (joined by sum_pieces_kernel)
+// weights' gradient: tiles of [d_in x d_out] per group, or, but for LARGE, per piece of `step` rows (joined by sum_pieces_kernel)
 template <typename T, Kind KIND, bool ODD>
 __global__ __launch_bounds__(kind_threads(KIND)) __attribute__((amdgpu_waves_per_eu(2))) void grouped_weight_kernel(const WeightArgs p)
 {
@@ -680,7 +691,7 @@ __global__ __launch_bounds__(kind_threads(KIND)) __attribute__((amdgpu_waves_per
     const int tiles = p.row_tiles * p.col_tiles, index = static_cast<int>(blockIdx.x) / tiles;
     Span s;
     Sink sink;
-    if (!weight_span(p, index, &s, &sink)) return;
+    if (!weight_span<KIND != LARGE>(p, index, &s, &sink)) return;
     int row, col;
     band_order(static_cast<int>(blockIdx.x) % tiles, p.row_tiles, p.col_tiles, kBandRows / BM, &row, &col);
     const int row0 = row * BM, col0 = col * BN;
@@ -736,7 +747,7 @@ __global__ __launch_bounds__(256) void tiny_weight_kernel(const WeightArgs p)
     const int tiles = p.row_tiles * p.col_tiles, index = static_cast<int>(blockIdx.x) / tiles;
     Span s;
     Sink sink;
-    if (!weight_span(p, index, &s, &sink)) return;
+    if (!weight_span<true>(p, index, &s, &sink)) return;
     const int64_t e = static_cast<int64_t>(blockIdx.x % tiles) * 256 + threadIdx.x;
     if (e >= static_cast<int64_t>(p.d_in) * p.d_out) return;
     const int k = static_cast<int>(e / p.d_out), n = static_cast<int>(e % p.d_out);
@@ -746,7 +757,7 @@ __global__ __launch_bounds__(256) void tiny_weight_kernel(const WeightArgs p)
 }
 
 // out[g] (+)= the sum of the partial sums of the group's pieces, `width` values each: the wavefronts of a block share them,
-// each front to back.  `whole`: what a group of one piece has is in `out` already.
+// each front to back.  `whole`: what a group of one piece has is in `out` already, and there are no partial sums of it.
 constexpr int kJoinWaves = 16, kJoinCols = 4;
 struct JoinArgs {
     const float *part;
@@ -784,7 +795,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void sum_pieces_kernel(const JoinA
     }
     if (p.whole && hi - lo <= p.step) return;
     // (overlapping groups could have more pieces than there is room for)
-    const int first = count_pieces(p.ptr, g, p.n_rows, p.step, p.most), count = min(pieces_in(hi - lo, p.step), p.most - first);
+    const int first = count_pieces(p.ptr, g, p.n_rows, p.step, p.most, p.whole ? 2 : 1), count = min(pieces_in(hi - lo, p.step), p.most - first);
     // four pieces at least to a wavefront; the wavefronts that are left take other columns
     int split = 1;
     while (split < kJoinWaves && count >= 8 * split) split *= 2;
@@ -901,6 +912,7 @@ struct GradPlan {
     int32_t step;                   // rows of a piece of the weights' gradient, 0: groups whole
     int64_t row_tiles, col_tiles;
     int64_t pieces, mask_pieces;    // at most
+    int64_t slots;                  // partial sums: pieces of groups longer than one piece, at most
     int32_t mask_step;
     int64_t ld_dz;
     size_t dz, part, bias_part, bytes;
@@ -925,6 +937,9 @@ GradPlan plan_grad(int64_t n_rows, int32_t n_groups, int32_t d_in, int32_t d_out
         const int64_t step = ceil_div(ceil_div(n_rows, ceil_div(2 * kCus, tiles)), 64) * 64;
         g.step = static_cast<int32_t>(step < 256 ? 256 : (step < (1 << 30) ? step : 1 << 30));
         g.pieces = n_rows / g.step + present;
+        // (ceil(c / step) is at most 2 floor(c / step) where c > step)
+        const int64_t full = n_rows / g.step;
+        g.slots = n_rows <= g.step ? 0 : (full < present ? 2 * full : full + present);
     }
     // some 2048 blocks of the mask, 64 rows and 64 x 16 bytes at least
     g.mask_step = static_cast<int32_t>(ceil_div(ceil_div(n_rows * ceil_div(d_out, 64 * chunk), 2048), 64) * 64);
@@ -933,7 +948,7 @@ GradPlan plan_grad(int64_t n_rows, int32_t n_groups, int32_t d_in, int32_t d_out
     g.ld_dz = static_cast<int64_t>(round_up(static_cast<size_t>(d_out), 8));
     size_t at = 0;
     g.dz = at; at += relu ? round_up(static_cast<size_t>(n_rows) * g.ld_dz * (dtype == MGG_BF16 ? 2 : 4), 256) : 0;
-    g.part = at; at += g.step ? round_up(static_cast<size_t>(g.pieces) * d_in * d_out * 4, 256) : 0;
+    g.part = at; at += round_up(static_cast<size_t>(g.slots) * d_in * d_out * 4, 256);
     g.bias_part = at; at += round_up(static_cast<size_t>(g.mask_pieces) * d_out * 4, 256);
     g.bytes = at + 256;
     return g;
@@ -1099,7 +1114,7 @@ mgg_status_t launch_update_grouped_grad(const GroupedGrad &q, void *workspace, h
     auto weights = [&](bool dry) {
         WeightArgs p{};
         p.a = q.a; p.dz = dz; p.ptr = q.group_ptr; p.n_rows = q.n_rows; p.ld_a = q.ld_a; p.ld_dz = ld_dz;
-        p.n_groups = q.n_groups; p.d_in = q.d_in; p.d_out = q.d_out; p.step = g.step;
+        p.n_groups = q.n_groups; p.d_in = q.d_in; p.d_out = q.d_out; p.step = g.step; p.slots = static_cast<int32_t>(g.slots);
         p.sink = Sink{q.grad_w, q.d_out, nullptr, q.d_out, q.grad_w_dtype == MGG_BF16, 0, q.add_w};
         p.part = reinterpret_cast<float *>(ws + g.part);
         return bf16 ? weight_product_of<Bf16>(p, g, dry, stream) : weight_product_of<float>(p, g, dry, stream);
@@ -1131,7 +1146,7 @@ mgg_status_t launch_update_grouped_grad(const GroupedGrad &q, void *workspace, h
         s = weights(false);
         if (s != MGG_OK || !g.step) return s;
         s = join_pieces(JoinArgs{reinterpret_cast<float *>(ws + g.part), q.group_ptr, q.grad_w, q.n_rows, static_cast<int64_t>(q.d_in) * q.d_out, q.n_groups, g.step,
-                                 static_cast<int32_t>(g.pieces), q.grad_w_dtype == MGG_BF16, q.add_w, 1}, stream);
+                                 static_cast<int32_t>(g.slots), q.grad_w_dtype == MGG_BF16, q.add_w, 1}, stream);
     }
     return s;
 }

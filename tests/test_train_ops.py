@@ -875,3 +875,40 @@ def test_one_group_of_few_rows_and_many_columns(n, tile):
     assert_within(binding.mgg_update_grouped(*args), ref, (d_in + 2) * U * mag + half_step(BF16) * ref.abs())
     out = torch.empty(n, d_out, dtype=BF16, device=DEV)
     assert launches(lambda: binding.mgg_update_grouped(*args, out=out)) == [((n // tile + 1) * (d_out // tile), 2 * tile)]
+
+
+def test_workspace_has_no_partial_sums_of_groups_that_are_one_piece():
+    """A matrix per piece only for groups longer than a piece: at most 2 floor(n / step) of them, 256 rows to a piece at least."""
+    grouped = binding.mgg_update_grouped_grad_workspace_bytes
+    bias = lambda n, groups, d_out: (n // 64 + min(n, groups)) * d_out * 4          # of the columns' sums, 64 rows to a piece at least
+    assert grouped(64, 64, 512, 1024, F32) <= bias(64, 64, 1024) + 1024
+    assert grouped(255, 5, 602, 47, F32) <= bias(255, 5, 47) + 1024
+    assert grouped(65536, 128, 1001, 1801, BF16) <= 8 * 1001 * 1801 * 4 + bias(65536, 128, 1801) + 1024           # (13,120 rows to a piece)
+    assert grouped(1000, 1, 64, 64, BF16) >= 4 * 64 * 64 * 4
+
+
+@gpu
+@pytest.mark.parametrize("dtype,d_in,d_out", [(BF16, 64, 64), (F32, 40, 72), (BF16, 3, 20), (BF16, 130, 47)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_weight_gradients_of_groups_of_one_piece_and_of_several(dtype, d_in, d_out, accumulate):
+    """150 groups of lengths about multiples of a piece (256 rows here), in a workspace of just the size that is asked for."""
+    rng = np.random.default_rng(d_in)
+    counts = rng.choice([0, 1, 255, 256, 257, 300, 512, 513, 1100], 150).tolist()
+    n, groups = sum(counts), len(counts)
+    g = torch.Generator().manual_seed(d_out)
+    a, dz, w = torch.randn(n, d_in, generator=g).to(dtype), torch.randn(n, d_out, generator=g).to(dtype), torch.zeros(groups, d_in, d_out, dtype=dtype)
+    into, into_b = torch.randn(groups, d_in, d_out, generator=g), torch.randn(groups, d_out, generator=g)
+    ptr = group_ptr(counts)
+    (_, dw, db), (_, mw, mb) = grouped_grad_reference(ptr, dz, a, w)
+    if accumulate:
+        dw, db, mw, mb = dw + into, db + into_b, mw + into.abs(), mb + into_b.abs()
+    need = binding.mgg_update_grouped_grad_workspace_bytes(n, groups, d_in, d_out, dtype)
+    buf = torch.full((need + 8192,), 0xff, dtype=torch.uint8, device=DEV)           # (NaN wherever it is read before it is written)
+    args = [t.to(DEV) for t in (ptr, dz, a, w)]
+    for _ in range(2):
+        _, gw, gb = binding.mgg_update_grouped_grad(*args, need_a=False, need_bias=True, grad_w=into.to(DEV), grad_bias=into_b.to(DEV), accumulate=accumulate,
+                                                    workspace=buf[4096: 4096 + need])
+        assert bool((buf[:4096] == 0xff).all()) and bool((buf[4096 + need:] == 0xff).all())
+        terms = (max(counts) + 3) * U
+        assert_within(gw, dw, terms * mw + half_step(F32) * dw.abs(), "grad_w")
+        assert_within(gb, db, terms * mb + half_step(F32) * db.abs(), "grad_bias")
