@@ -729,7 +729,7 @@ def mgg_update_grouped_grad(group_ptr, grad_out, a, w, act: str = "none", *, out
                             grad_a=None, grad_w=None, grad_bias=None, w_grad_dtype=None, accumulate: bool = False, workspace=None, stream=None):
     """Gradients of mgg_update_grouped: (grad_a, grad_w), and grad_bias behind them with need_bias; None in the place of one that
     is not needed.  `out` is what the forward call wrote (act "relu" only).  grad_a has a's dtype, grad_w fp32 unless
-    `w_grad_dtype` says otherwise; accumulate adds to the grad_w and grad_bias that are given."""
+    `w_grad_dtype` says otherwise; accumulate adds to the grad_w and grad_bias that are given (one at least), others are written anew."""
     import torch
     n_groups = int(group_ptr.shape[0]) - 1
     _check_groups(group_ptr, w, n_groups)
@@ -742,6 +742,8 @@ def mgg_update_grouped_grad(group_ptr, grad_out, a, w, act: str = "none", *, out
         raise ValueError("the gradient of a ReLU needs the forward call's `out`")
     if act == "relu":
         _shape("out", out, n, d_out)
+    if accumulate and grad_w is None and grad_bias is None:
+        raise ValueError("accumulate needs `grad_w` or `grad_bias`")
     _same_device(group_ptr, grad_out, a, w, out if act == "relu" else None, grad_a, grad_w, grad_bias, workspace)
     add = (ACC_W if accumulate and grad_w is not None else 0) | (ACC_BIAS if accumulate and grad_bias is not None else 0)
     if need_a and grad_a is None:

@@ -912,3 +912,12 @@ def test_weight_gradients_of_groups_of_one_piece_and_of_several(dtype, d_in, d_o
         terms = (max(counts) + 3) * U
         assert_within(gw, dw, terms * mw + half_step(F32) * dw.abs(), "grad_w")
         assert_within(gb, db, terms * mb + half_step(F32) * db.abs(), "grad_bias")
+
+
+def test_accumulating_into_nothing_is_refused():
+    ptr, a, w = torch.zeros(3, dtype=torch.int64), torch.zeros(4, 8), torch.zeros(2, 8, 8)
+    with pytest.raises(ValueError, match="accumulate"):
+        binding.mgg_update_grouped_grad(ptr, a, a, w, need_bias=True, accumulate=True)
+    for given in (dict(grad_w=torch.zeros(2, 8, 8)), dict(grad_bias=torch.zeros(2, 8))):         # (these go on to the refusal of host tensors)
+        with pytest.raises(TypeError):
+            binding.mgg_update_grouped_grad(ptr, a, a, w, need_bias=True, accumulate=True, **given)
