@@ -28,7 +28,7 @@ struct DistillArgs {
     const float *row_weight;
     float *loss;
     void *grad;
-    float *stats;           // pieces: [rows x (2 pieces + 4)]
+    float *stats;           // pieces: [rows x (2 pieces + 3)]: what piece 0 knows, then a maximum and a sum each
     int64_t n_rows, ld_logits, ld_ids, ld_top, ld_grad;
     int32_t n_classes, k;
     float temperature, inv_t;
@@ -380,7 +380,7 @@ __global__ __launch_bounds__(kPieceThreads) void distill_stats_kernel(const Dist
         if (ONE && threadIdx.x == 0) p.loss[row] = 0.f;
         return;
     }
-    float *stats = p.stats + row * (2 * static_cast<int64_t>(p.pieces) + 4);
+    float *stats = p.stats + row * (2 * static_cast<int64_t>(p.pieces) + 3);
     const int64_t lo = index * p.piece, hi = lo + p.piece < p.n_classes ? lo + p.piece : p.n_classes;
     Running top{-INFINITY, 0.f};
     if (index == 0) top = teacher_load<In, kPieceThreads>(p, row, z, t, c2);
@@ -404,7 +404,7 @@ __global__ __launch_bounds__(kPieceThreads) void distill_stats_kernel(const Dist
         r.s = s;
     }
     r = block_join<kPieceThreads>(r, c2, part);
-    if (!ONE && threadIdx.x == 0) { stats[4 + 2 * index] = r.m; stats[5 + 2 * index] = r.s; }
+    if (!ONE && threadIdx.x == 0) { stats[3 + 2 * index] = r.m; stats[4 + 2 * index] = r.s; }
     if (index != 0) return;
     top = block_join<kPieceThreads>(top, c2, part);
     const bool none = top.m == -INFINITY && top.s == 0.f;
@@ -420,7 +420,7 @@ __global__ __launch_bounds__(kPieceThreads) void distill_stats_kernel(const Dist
         ref = block_join<kPieceThreads>(ref, c2, part);
         const float at = ref.m == -INFINITY ? 0.f : ref.m;
         const float loss = none ? 0.f : block_sum<kPieceThreads>(teacher_loss<kPieceThreads>(p, t, top, at, c2), part);
-        if (threadIdx.x == 0) { stats[0] = loss; stats[1] = at; stats[2] = none ? 1.f : 0.f; stats[3] = top.m; }
+        if (threadIdx.x == 0) { stats[0] = loss; stats[1] = at; stats[2] = none ? 1.f : 0.f; }
     }
 }
 
@@ -435,11 +435,11 @@ __global__ __launch_bounds__(kPieceThreads) void distill_pieces_kernel(const Dis
     const In *z = static_cast<const In *>(p.logits) + row * p.ld_logits;
     Out *dz = static_cast<Out *>(p.grad) + row * p.ld_grad;
     const float weight = p.row_weight ? p.row_weight[row] : 1.f, c2 = p.inv_t * kLog2e;
-    const float *stats = p.stats + row * (2 * static_cast<int64_t>(p.pieces) + 4);
+    const float *stats = p.stats + row * (2 * static_cast<int64_t>(p.pieces) + 3);
     Running r{-INFINITY, 0.f};
     bool empty = weight == 0.f;
     if (!empty) {
-        for (int i = threadIdx.x; i < p.pieces; i += kPieceThreads) r.join(stats[4 + 2 * i], stats[5 + 2 * i], c2);
+        for (int i = threadIdx.x; i < p.pieces; i += kPieceThreads) r.join(stats[3 + 2 * i], stats[4 + 2 * i], c2);
         r = block_join<kPieceThreads>(r, c2, part);
         empty = stats[2] != 0.f || (r.m == -INFINITY && r.s == 0.f);
     }
@@ -481,33 +481,36 @@ __global__ __launch_bounds__(kPieceThreads) void distill_pieces_kernel(const Dis
     teacher_grad<Out, kPieceThreads>(p, t, dz, lo, hi, r.m, inv_s, factor, c2);
 }
 
-// Pieces of a row where it is taken in pieces: workgroups enough for the chip, 4096 classes at least.
+// Pieces of a row where it is taken in pieces: workgroups enough for the chip, but not more pieces than there are 4096 classes, begun
+// ones counted (4097 classes are two pieces of some 2 k).
 int pieces_of(int64_t n_rows, int32_t n_classes)
 {
     const int64_t wanted = n_rows < 2048 ? ceil_div(2048, n_rows > 0 ? n_rows : 1) : 1, most = ceil_div(n_classes, 4096);
     return static_cast<int>(wanted < most ? wanted : most);
 }
 
+// The longest rows, in vectors, that the registers of a workgroup hold, and those that are short.
+constexpr int kShortVecs = kWave * kShortMax, kRow256Vecs = 256 * 8, kRow1024Vecs = 1024 * 16;
+
+// rows of more than kShortVecs vectors, with a gradient, by 256 or 1024 threads
 template <typename In, typename Out, int THREADS>
-bool launch_rows(const DistillArgs &p, hipStream_t stream)
+void launch_rows(const DistillArgs &p, hipStream_t stream)
 {
     const dim3 grid(static_cast<unsigned>(p.n_rows)), block(THREADS);
     const int64_t per = ceil_div(ceil_div(p.n_classes, Vec<In>::N), THREADS);
 #define MGG_ROWS(NV) hipLaunchKernelGGL((distill_row_kernel<In, Out, THREADS, NV>), grid, block, 0, stream, p)
     if constexpr (THREADS == 256) {
-        if (per <= 1) MGG_ROWS(1);
-        else if (per <= 2) MGG_ROWS(2);
+        static_assert(kShortVecs >= 256 && kRow256Vecs == 256 * 8, "two to eight vectors of a thread");
+        if (per <= 2) MGG_ROWS(2);
         else if (per <= 4) MGG_ROWS(4);
-        else if (per <= 8) MGG_ROWS(8);
-        else return false;
+        else MGG_ROWS(8);
     } else {
+        static_assert(THREADS == 1024 && kRow1024Vecs == 1024 * 16, "up to sixteen");
         if (per <= 4) MGG_ROWS(4);
         else if (per <= 8) MGG_ROWS(8);
-        else if (per <= 16) MGG_ROWS(16);
-        else return false;
+        else MGG_ROWS(16);
     }
 #undef MGG_ROWS
-    return true;
 }
 
 template <typename In, typename Out>
@@ -516,7 +519,7 @@ mgg_status_t launch_typed(DistillArgs p, hipStream_t stream)
     constexpr int N = Vec<In>::N;
     const char *const refused = "too many rows for one launch";
     const int64_t vecs = ceil_div(p.n_classes, N);
-    if (vecs <= kWave * kShortMax) {
+    if (vecs <= kShortVecs) {
         // four lanes at least, which share the teacher's entries; four vectors at most per lane
         p.lanes_log2 = ceil_log2(ceil_div(vecs, kShortMax));
         if (p.lanes_log2 < 2) p.lanes_log2 = 2;
@@ -527,10 +530,10 @@ mgg_status_t launch_typed(DistillArgs p, hipStream_t stream)
         else if (per <= 2) hipLaunchKernelGGL((distill_short_kernel<In, Out, 2>), grid, dim3(kShortThreads), 0, stream, p);
         else if (per <= 3) hipLaunchKernelGGL((distill_short_kernel<In, Out, 3>), grid, dim3(kShortThreads), 0, stream, p);
         else hipLaunchKernelGGL((distill_short_kernel<In, Out, 4>), grid, dim3(kShortThreads), 0, stream, p);
-    } else if (p.grad && vecs <= 8 * 256) {
+    } else if (p.grad && vecs <= kRow256Vecs) {
         if (!launchable(p.n_rows, 256)) return fail(MGG_ERR_UNSUPPORTED, "%s", refused);
         launch_rows<In, Out, 256>(p, stream);
-    } else if (p.grad && vecs <= 16 * 1024 && (p.n_rows >= 64 || vecs <= 4 * 1024)) {
+    } else if (p.grad && vecs <= kRow1024Vecs && (p.n_rows >= 64 || vecs <= 4 * 1024)) {
         // (100 rows of 128 k bf16: 31 us, in pieces 35; 16 rows: 28 and 21; 4 rows of 30 k: 13 and 17)
         if (!launchable(p.n_rows, 1024)) return fail(MGG_ERR_UNSUPPORTED, "%s", refused);
         launch_rows<In, Out, 1024>(p, stream);
@@ -556,7 +559,7 @@ mgg_status_t launch_typed(DistillArgs p, hipStream_t stream)
 
 size_t distill_workspace(int64_t n_rows, int32_t n_classes)
 {
-    return static_cast<size_t>(n_rows) * (2 * static_cast<size_t>(pieces_of(n_rows, n_classes)) + 4) * 4 + 256;
+    return static_cast<size_t>(n_rows) * (2 * static_cast<size_t>(pieces_of(n_rows, n_classes)) + 3) * 4 + 256;
 }
 
 mgg_status_t launch_distill(const Distill &q, void *workspace, hipStream_t stream)
