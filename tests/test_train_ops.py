@@ -393,9 +393,9 @@ def test_grouped_gradients(counts, d_in, d_out, dtype, tw, act, accumulate):
 # Sizes at which the kernels for many rows run: (counts, d_in, d_out, dtype).  Ends inside tiles and inside 16 bytes, empty groups, groups
 # shorter than a tile beside long ones.
 MANY = [
-    ([4000, 0, 1, 4700, 299], 200, 2048, BF16),         # whole chunks: large tiles forward; d_out long: large tiles of the weights' gradient, too
+    ([4000, 0, 1, 4700, 299], 200, 2048, BF16),         # whole chunks: large tiles forward; medium ones of the weights' gradient
     ([4000, 0, 1, 4700, 299], 2048, 200, BF16),         # large tiles of the rows' gradient
-    ([64] * 9 + [0, 130, 3] + [70] * 8, 1024, 1032, BF16),
+    ([64] * 9 + [0, 130, 3] + [70] * 8, 1024, 1032, BF16),       # large tiles of the weights' gradient, up to three steps
     ([2500, 7, 2493], 203, 1001, BF16),
     ([2500, 7, 2493], 1001, 203, BF16),
     ([12000, 1, 8000], 130, 47, BF16),
@@ -921,3 +921,90 @@ def test_accumulating_into_nothing_is_refused():
     for given in (dict(grad_w=torch.zeros(2, 8, 8)), dict(grad_bias=torch.zeros(2, 8))):         # (these go on to the refusal of host tensors)
         with pytest.raises(TypeError):
             binding.mgg_update_grouped_grad(ptr, a, a, w, need_bias=True, accumulate=True, **given)
+
+
+# ---- kernels at lengths where their loops come round ----------------------------------------------------------
+STEPS = [64, 72, 128, 136, 192, 200, 256, 320, 328, 512, 1000]      # a step of the sum is 64 long
+
+
+@gpu
+@pytest.mark.parametrize("depth", STEPS)
+def test_large_tiles_over_one_to_many_steps(depth):
+    """256 x 256 tiles of the forward product and of the rows' gradient (a block has 512 threads there): sums of one step, of two to
+    sixteen, whole and with a remainder, over groups that end in and at tiles."""
+    counts, wide = [1500, 0, 700, 1, 255, 256, 257, 1031], 2056
+    n, groups = sum(counts), len(counts)
+    g = torch.Generator().manual_seed(depth)
+    a, w = torch.randn(n, depth, generator=g).bfloat16(), (torch.randn(groups, depth, wide, generator=g) * depth ** -0.5).bfloat16()
+    ptr, bias = group_ptr(counts), torch.randn(groups, wide, generator=g)
+    grid = [((n // 256 + groups) * 9, 512)]
+    ref, mag = grouped_reference(ptr, a, w, bias, "none")
+    args = (ptr.to(DEV), a.to(DEV), w.to(DEV), bias.to(DEV))
+    out = torch.empty(n, wide, dtype=F32, device=DEV)
+    assert_within(binding.mgg_update_grouped(*args, out=out), ref, (depth + 2) * U * mag + half_step(F32) * ref.abs(), "out")
+    assert launches(lambda: binding.mgg_update_grouped(*args, out=out)) == grid
+    # the same product as a rows' gradient: dz = a, the weights turned
+    turned, rows = w.transpose(1, 2).contiguous().to(DEV), torch.zeros(n, wide, dtype=BF16, device=DEV)
+    call = dict(need_w=False, grad_a=out, workspace=torch.empty(binding.mgg_update_grouped_grad_workspace_bytes(n, groups, wide, depth, BF16), dtype=torch.uint8, device=DEV))
+    ref, mag = grouped_reference(ptr, a, w, None, "none")
+    got, _ = binding.mgg_update_grouped_grad(args[0], args[1], rows, turned, **call)
+    assert_within(got, ref, (depth + 2) * U * mag + half_step(F32) * ref.abs(), "grad_a")
+    assert launches(lambda: binding.mgg_update_grouped_grad(args[0], args[1], rows, turned, **call)) == grid
+
+
+@gpu
+@pytest.mark.parametrize("tw,accumulate", [(F32, False), (F32, True), (BF16, False)])
+def test_large_tiles_of_weight_gradients_over_none_to_many_steps(tw, accumulate):
+    """Groups of 0 to 1000 rows, a step being 64 of them: exactly one to seven steps, and with a remainder."""
+    counts, d_in, d_out = [1000, 192, 128, 256, 64, 320, 0, 1, 63, 65, 129, 7, 0, 200, 384, 449, 72, 500, 130, 191], 1024, 1032
+    n, groups = sum(counts), len(counts)
+    g = torch.Generator().manual_seed(7)
+    a, dz = torch.randn(n, d_in, generator=g).bfloat16(), torch.randn(n, d_out, generator=g).bfloat16()
+    into = torch.randn(groups, d_in, d_out, generator=g).to(tw)
+    ptr, w = group_ptr(counts), torch.zeros(groups, d_in, d_out, dtype=BF16)
+    (_, ref, _), (_, mag, _) = grouped_grad_reference(ptr, dz, a, w)
+    if accumulate:
+        ref, mag = ref + into, mag + into.abs()
+    args = [t.to(DEV) for t in (ptr, dz, a, w)]
+    call = dict(need_a=False, grad_w=into.to(DEV), accumulate=accumulate,
+                workspace=torch.empty(binding.mgg_update_grouped_grad_workspace_bytes(n, groups, d_in, d_out, BF16), dtype=torch.uint8, device=DEV))
+    got = binding.mgg_update_grouped_grad(*args, **call)[1]
+    assert_within(got, ref, (torch.tensor(counts)[:, None, None] + 3) * U * mag + half_step(tw) * ref.abs(), "grad_w")
+    assert launches(lambda: binding.mgg_update_grouped_grad(*args, **call)) == [(groups * 4 * 5, 512)]
+
+
+@gpu
+@pytest.mark.parametrize("d_in,d_out", [(256, 1024), (250, 1001), (1000, 1500)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_row_or_two_to_each_of_many_groups(d_in, d_out, dtype):
+    """Four wavefronts share the sum of a tile of 32 rows where there are 512 tiles and more: a serving step over 64 groups, 23 of them idle."""
+    rng = np.random.default_rng(d_in)
+    counts = np.bincount(rng.permutation(64)[rng.integers(0, 41, 64)], minlength=64).tolist()
+    n, groups = sum(counts), len(counts)
+    g = torch.Generator().manual_seed(d_out)
+    a, dz = torch.randn(n, d_in, generator=g).to(dtype), torch.randn(n, d_out, generator=g).to(dtype)
+    w, ptr = (torch.randn(groups, d_in, d_out, generator=g) * d_in ** -0.5).to(dtype), group_ptr(counts)
+    args = [t.to(DEV) for t in (ptr, dz, a, w)]
+    ref, mag = grouped_reference(ptr, a, w, None, "none")
+    out = torch.empty(n, d_out, dtype=dtype, device=DEV)
+    assert_within(binding.mgg_update_grouped(args[0], args[2], args[3], out=out), ref, (d_in + 2) * U * mag + half_step(dtype) * ref.abs(), "out")
+    assert launches(lambda: binding.mgg_update_grouped(args[0], args[2], args[3], out=out)) == [((n // 32 + 64) * -(-d_out // 64), 256)]
+    refs, mags = grouped_grad_reference(ptr, dz, a, w)
+    for name, x, r, m, k in zip(("grad_a", "grad_w"), binding.mgg_update_grouped_grad(*args), refs, mags, (d_out, max(counts))):
+        assert_within(x, r, (k + 3) * U * m + half_step(x.dtype) * r.abs(), name)
+
+
+@gpu
+@pytest.mark.parametrize("n,classes,k,dtype,shape", [(64, 40001, 7, F32, (64, 1024)), (66, 65536, 3, F32, (66, 1024)), (64, 131072, 5, BF16, (64, 1024)),
+                                                     (65, 65544, 9, BF16, (65, 1024)), (3, 16384, 4, F32, (3, 1024)), (3, 8192, 4, F32, (3, 256)), (4, 8193, 4, F32, (4, 1024)),
+                                                     (5, 1025, 3, F32, (5, 256)), (5, 2049, 3, BF16, (5, 256))])
+def test_distill_rows_at_the_ends_of_what_registers_hold(n, classes, k, dtype, shape):
+    z, ids, top, weight = draw_distill(n, classes, k, classes, dtype, F32)
+    loss, grad, loss_bound, grad_bound = distill_reference(z, ids, top, 2.0, weight)
+    args = [t.to(DEV) for t in (z, ids, top)]
+    call = dict(temperature=2.0, row_weight=weight.to(DEV), loss=torch.empty(n, device=DEV), grad=torch.empty(n, classes, dtype=dtype, device=DEV),
+                workspace=torch.empty(binding.mgg_distill_workspace_bytes(n, classes), dtype=torch.uint8, device=DEV))
+    got, got_grad = binding.mgg_distill_loss(*args, **call)
+    assert_within(got, loss, loss_bound + half_step(F32) * loss.abs(), "loss")
+    assert_within(got_grad, grad, grad_bound + half_step(dtype) * grad.abs() + 1e-37, "gradient")
+    assert launches(lambda: binding.mgg_distill_loss(*args, **call)) == [shape]
