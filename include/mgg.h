@@ -412,7 +412,8 @@ mgg_status_t mgg_embed_grad(int64_t n, mgg_index_t id_type, const void *ids, int
  * [0, n_rows]; offsets outside are taken as the nearest bound and a group whose end lies before its start as empty, so
  * that no access leaves the buffers, but which rows of groups that overlap are written is then not defined.  Rows
  * before the first group and behind the last are left as they were and are part of no sum; an empty group
- * has a grad_w and grad_bias of zeros.  n_groups 1 with {0, n_rows} is the plain Update of mgg_update.
+ * has a grad_w and grad_bias of zeros.  n_groups 1 with {0, n_rows} is the Update of mgg_update by other kernels, whose sums have
+ * another order: last bits differ, and for many rows in F32 mgg_update is faster and closer (it multiplies in bf16 parts).
  * a [n_rows x d_in], w [n_groups x d_in x d_out] contiguous, grad_out [n_rows x d_out]: DEVICE, one dtype for all, F32 or
  * BF16.  bias, grad_bias [n_groups x d_out] DEVICE fp32 or NULL.  out, grad_a [n_rows x d_in], grad_w (like w): F32 or
  * BF16 each.  Products are summed in fp32 (F32 operands on the fp32 matrix instruction) and rounded once as they
@@ -459,7 +460,9 @@ mgg_status_t mgg_update_grouped_grad(int64_t n_rows, int32_t n_groups, const int
  * left, and where all its logits are -infinity.  A class with logit -infinity has q = 0; the loss is infinite where the
  * teacher gives it p > 0.  NaN or +infinity elsewhere give NaN in their row.
  * loss [n_rows] DEVICE fp32.  grad_logits [n_rows x n_classes] F32 or BF16, or NULL: no gradient; it may be `logits`
- * itself (same dtype and leading dimension) and must not overlap it otherwise.  Arithmetic is fp32, in a fixed order.
+ * itself (same dtype and leading dimension) and must not overlap it otherwise.  Arithmetic is fp32, in a fixed order; the
+ * two logarithms are off by up to some 2^-21 of 1 and of their size, the loss by w T^2 times that, which at temperatures of several
+ * hundred is no longer little beside a loss that stays near the logits' variance (a teacher that keeps all classes).
  * workspace: a DEVICE buffer of at least mgg_distill_workspace_bytes() bytes, 256-byte aligned, that no other call uses
  * at the same time.  Asynchronous on `stream`, allocates nothing, can be captured into a graph.
  * Errors: INVALID_ARG (a temperature outside [1e-6, 1e6] among them), UNSUPPORTED (k above 1024, 2^31 - 1 classes

@@ -589,7 +589,8 @@ def mgg_layer_forward(part: Partition, mode: str, x_local, x_halo, weights, acts
 
 # ------------------------------------------------------------------------------- training
 # Lookup, grouped Update and distillation loss.  What the C ABI cannot see is checked here: shapes, dtypes, and that every
-# tensor lives on the current device (whose stream the call goes to).
+# tensor lives on the current device (whose stream the call goes to).  Outputs carry no autograd history, whatever the inputs
+# require: gradients are calls of their own.
 def _same_device(*tensors):
     lib()                       # (torch is there from here on)
     first = tensors[0].get_device()

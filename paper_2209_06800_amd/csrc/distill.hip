@@ -9,7 +9,9 @@
 //   - few rows, or longer ones: pieces of rows; each piece's maximum and sum first, then the gradient from a second reading
 //     (out of the caches where it is for few rows).
 // 4096 rows of 128 k bf16 with gradient: 0.47 ms, 1.99 GB at 4.2 TB/s, the row in the registers of 1024 threads (a block per row that
-// reads it three times: 1.84 ms); 306 k rows of 47 fp32, loss alone: 22 us, 3.2 TB/s; 37 rows of 50 k with gradient: 16 us, two launches.
+// reads it three times: 1.84 ms); 306 k rows of 47 fp32: loss alone 27 us, 2.7 TB/s, with gradient 49 us, 2.8 TB/s; 37 rows of 50 k with gradient:
+// 17 us, two launches; 2000 rows with gradient in pieces, read twice: 151,936 bf16 345 us, 262,144 bf16 577, 128,000 fp32 549 (1.16, 1.99 and 1.95 GB
+// at 3.4 - 3.5 TB/s, once counted); 4096 rows of 128 k bf16, loss alone: 174 us, 5.4 TB/s.
 #include <cmath>
 
 #include "train_common.h"

@@ -16,7 +16,9 @@
 //   - few rows to a group: reading the weights.  64 rows over 64 groups 1024 -> 2048 bf16, 41 of them with rows: 38 us, 172 MB at 4.6 TB/s
 //     (30 where the Infinity Cache still holds a part).
 //   - short sums (widths up to some hundred): the chain of a block from its group's offsets over its operands to its stores, a few
-//     microseconds for each of the rounds that fill the chip.  233 k rows 100 -> 256 fp32: 181 - 192 us, where bytes and instructions allow 77.
+//     microseconds for each of the rounds that fill the chip.  233 k rows 100 -> 256 fp32: 181 - 192 us, where bytes and instructions allow 77;
+//     60 k rows 300 -> 200 bf16 over 7 groups: 36 us, bytes allow 12.
+//   - widths below 16 bytes: plain sums, one result per thread, bound by the latency of loads a row apart (tiny_rows_kernel).
 #include "train_common.h"
 
 namespace mgg {
@@ -707,6 +709,8 @@ __global__ __launch_bounds__(kind_threads(KIND)) __attribute__((amdgpu_waves_per
 }
 
 // ---- widths of less than 16 bytes: plain sums ------------------------------------------------------------------
+// 100 k rows over 5 groups: 500 -> 3 fp32 368 us forward (201 MB, which HBM allows in 39), 120 and 451 for the gradients of rows and weights;
+// 64 -> 7 bf16 85, 39 and 183.
 __device__ __forceinline__ void put1(const Sink &p, float v, int64_t row, int col)
 {
     if (p.bias) v += p.bias[col];

@@ -342,8 +342,9 @@ __global__ __launch_bounds__(kThreads) void sort_scatter_kernel(const SortArgs p
 // costs no more than others.  A chunk's rows are added up id by id; a sum that began and ended inside the chunk is a
 // finished row, one that reaches over its border goes to the workspace (slot 0 of the chunk: it began before; slot 1: it goes on), and
 // embed_join_kernel adds those up chunk by chunk.  Bound by HBM: the rows of grad_out read once, grad_table written once.  32 k ids over
-// 128 k rows of 2048, bf16 to fp32: the sums and zeros 185 - 220 us (1.17 GB at 5.3 - 6.3 TB/s), the sort 30, the join 12.  Stores that pass the
-// caches by took 14 % longer in all (277 to 317 us, before the zeros went in larger shares).
+// 128 k rows of 2048, bf16 to fp32: the sums and zeros 185 - 220 us (1.17 GB at 5.3 - 6.3 TB/s), the sort 30, the join 12.  1 M ids over
+// 100 k rows of 64 fp32: 65, the sort 87 (40 of them its two scans), the join 20, where bytes allow 53 in all.  Stores that pass the caches by took
+// 14 % longer in all (277 to 317 us, before the zeros went in larger shares).
 constexpr int chunk_of(int64_t n) { return n <= 4096 ? 8 : (n <= 16384 ? 16 : (n <= 262144 ? 32 : 64)); }     // enough chunks for the chip, few partial sums
 
 struct EmbedGradPlan {
