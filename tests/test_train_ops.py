@@ -1043,3 +1043,22 @@ def test_a_training_step_around_the_aggregation():
     for name, x, ref in zip(("loss", "table", "w1", "b1", "w2"), (loss, dtable, dw1, db1, dw2[0]), [want.detach()] + [leaf.grad for leaf in leaves]):
         rel = float((x.double().cpu() - ref).norm() / ref.norm())
         assert rel < 7 * 700 * U, (name, rel)
+
+
+@gpu
+@pytest.mark.parametrize("offsets", [[0, 2000, 500, 2000], [0, 2000] * 40, [0, 2000, 1999, 3, 1500, 0, 5000, -7, 700]])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_overlapping_groups_of_several_pieces_stay_inside_the_workspace(offsets, dtype):
+    """Such groups have more pieces than ascending offsets could have; what they compute is not defined, where it is written is."""
+    n, d, groups = 2000, 24, len(offsets) - 1
+    ptr = torch.tensor(offsets, device=DEV)
+    one = lambda *shape: torch.ones(*shape, dtype=dtype, device=DEV)
+    need = binding.mgg_update_grouped_grad_workspace_bytes(n, groups, d, d, dtype, act="relu")
+    space, around = torch.full((need + 8192,), 0x3c, dtype=torch.uint8, device=DEV), torch.full((3 * n, d), 5.0, dtype=dtype, device=DEV)
+    around_w = torch.full((3 * groups, d, d), 5.0, device=DEV)
+    binding.mgg_update_grouped_grad(ptr, one(n, d), one(n, d), one(groups, d, d), "relu", out=one(n, d), need_bias=True, grad_a=around[n:2 * n],
+                                    grad_w=around_w[groups:2 * groups], workspace=space[4096: 4096 + need])
+    torch.cuda.synchronize()
+    assert bool((space[:4096] == 0x3c).all()) and bool((space[4096 + need:] == 0x3c).all())
+    assert bool((around[:n] == 5).all()) and bool((around[2 * n:] == 5).all())
+    assert bool((around_w[:groups] == 5).all()) and bool((around_w[2 * groups:] == 5).all())
